@@ -13,6 +13,11 @@
  *   a6  lsa_sparse_attn   attention over sink U window U sparse     Eq. 3, Sec. 4.1.1
  *   a7  lsa_layer_group   a0..a5 once, a6 for each of the R layers  Sec. 3.2
  *
+ * Beside it, for the dense layers of the same model and for models whose caches have heads of their own:
+ *
+ *   lsa_kv_append         new keys and values into the rows of a paged cache, keys and queries rotated to their positions
+ *   lsa_paged_attn        attention of one new token per sequence over its whole paged cache, or over sink and window
+ *
  * Conventions
  *   - Positions are 0-indexed.  Query t sees keys s <= t.  S = k_sink, W = k_swa, Ksp = k_sparse.
  *     Candidate range of query t: C(t) = [S, t-W] (empty when t-W < S).  sink = [0, min(S,t+1)),
@@ -65,7 +70,8 @@ typedef enum {
                               paper_2608_01662_b200.build --check`): an attention kernel met a cache row number
                               outside [0, n_key) in a caller-given sparse list or row list; the row was skipped (it
                               contributes nothing) and the code is reported through lsa_status.  The normal build
-                              trusts these lists, as it trusts its pointers */
+                              trusts these lists, as it trusts its pointers.  lsa_kv_append and lsa_paged_attn check
+                              lengths, positions and page numbers in every build and report them with this code */
 } lsa_error;
 
 enum { LSA_KEY_BF16 = 0, LSA_KEY_E4M3 = 1 };
@@ -357,6 +363,84 @@ LSA_API int lsa_layer_group_host(lsa_ctx* ctx, const lsa_params* p, const void* 
                          const void* const* v, int64_t ld_k, int64_t ld_v, void* const* out_host,
                          int64_t stage_queries, void* const* stage, size_t stage_bytes);
 LSA_API int lsa_host_stage_bytes(const lsa_params* p, int64_t stage_queries, size_t* bytes);
+
+/* ---- paged key-value caches without an indexer ------------------------------------------------ */
+
+/* The layers of a model that attend every cached token (or a sink and a sliding window) beside the sparse ones.  A cache
+ * is a pool of rows, one per token: row = page_table[b][pos / kv_page] * kv_page + pos % kv_page, as in the paged mode of
+ * the path above.  Two kinds:
+ *   latent = 1   one row of 576 elements per token, shared by all query heads; its first 512 are the value (absorbed
+ *                MLA, the same rows lsa_sparse_attn reads).  1 to 64 query heads; kv_page 64, 128 or 256.
+ *   latent = 0   rows of n_kv_heads keys and rows of n_kv_heads values, each head d_qk = d_v = 64 or 128 elements;
+ *                query head h reads KV head h / (n_heads / n_kv_heads), at most 16 query heads each; kv_page 16, 32, 64,
+ *                128 or 256.  Elements of the cache: dtype, or OCP e4m3 codes with one fp32 scale per row and KV head.
+ * Plain data; set struct_size = sizeof(lsa_kv_params). */
+typedef struct {
+  uint32_t struct_size;
+  int32_t dtype;             /* LSA_DTYPE_BF16 or LSA_DTYPE_FP16: queries, new keys and values, outputs, plain caches */
+  int32_t cache_e4m3;        /* 0: caches hold dtype; 1: e4m3 codes (latent = 0 only) */
+  int32_t latent;
+  int32_t n_heads;           /* query heads */
+  int32_t n_kv_heads;        /* divides n_heads; 1 for latent caches */
+  int32_t d_qk;
+  int32_t d_v;
+  int32_t kv_page;           /* tokens per cache page */
+  int32_t d_rope;            /* dims of a query or key head that are rotated: 0, or a multiple of 16 */
+  int32_t rope_at;           /* the first of them, a multiple of 16; rope_at + d_rope <= d_qk */
+  int32_t rope_interleaved;  /* pairs: 0: dims (j, j + d_rope / 2), 1: dims (2j, 2j + 1) of the rotated part */
+  int32_t k_sink;            /* with k_swa > 0: the first k_sink tokens are seen too */
+  int32_t k_swa;             /* the last k_swa tokens are seen, the new one among them; 0: all are */
+  float sm_scale;            /* logits = sm_scale * q.k */
+} lsa_kv_params;
+
+enum { LSA_DTYPE_BF16 = 0, LSA_DTYPE_FP16 = 1 };
+
+/* Scratch of lsa_paged_attn with these parameters (lsa_kv_append needs the 256 bytes of the status words only): partial
+ * results of the parts that a cache's length is split into.  It does not grow with the batch.  Writes *bytes (host). */
+LSA_API int lsa_kv_workspace_bytes(const lsa_kv_params* p, size_t* bytes);
+
+/* New tokens into the cache.  Token i of sequence b goes to position pos = ctx_len[b] + i - its sequence's first token; its key
+ * is rotated: a pair (x, y) of the rotated dims with angle j becomes (x cos - y sin, y cos + x sin) in fp32, rounded once.
+ *   k_new      [n_tok, n_kv_heads, d_qk] rows of ld_k_new elements per token (heads contiguous)
+ *   v_new      [n_tok, n_kv_heads, d_v] rows of ld_v_new; NULL for latent caches
+ *   q, q_out   optional (both or neither): [n_tok, n_heads, d_qk] rows of ld_q / ld_q_out; q_out = q with the same dims
+ *              rotated.  q_out == q (and the same pitch) rotates in place; they must not overlap otherwise
+ *   n_tok      rows of k_new.  tok_start = NULL: one token per sequence, n_tok = batch.  Else int32 [batch + 1]: the tokens
+ *              of sequence b are tok_start[b] .. tok_start[b + 1] - 1 (ascending; a sequence may have none); rows outside
+ *              tok_start[0] .. tok_start[batch] - 1 are padding and are neither read for their values nor written
+ *   cos_sin    fp32 [n_pos, d_rope]: the cosines, then the sines, of position pos's d_rope / 2 angles; NULL iff d_rope = 0
+ *   k_pool, v_pool   [n_pages * kv_page] rows of ld_k / ld_v elements; v_pool NULL for latent caches
+ *   k_scale, v_scale  fp32 [n_pages * kv_page, n_kv_heads], e4m3 caches only: written with the codes.  Scale = amax / 448 of
+ *              the head's rotated fp32 values (1 for a zero row), code = round-to-nearest-even of value / scale, saturating
+ *   page_table int32 [batch, page_table_stride]; every page that the new tokens reach must be in it
+ *   ctx_len    int32 [batch]: lengths BEFORE the call.  ctx_len_out: optional int32 [batch], the lengths after it; may be
+ *              ctx_len itself
+ * A length below 0, a position outside the table or the angles, or a page number outside [0, n_pages) leaves that token's
+ * outputs as they were and is reported as LSA_ERR_INDEX by lsa_status; the other tokens are served.  Two tokens of a call must not
+ * share a row.  One launch (two where tok_start is given and ctx_len_out overlaps ctx_len). */
+LSA_API int lsa_kv_append(lsa_ctx* ctx, const lsa_kv_params* p, const void* k_new, int64_t ld_k_new, const void* v_new,
+                          int64_t ld_v_new, const void* q, int64_t ld_q, void* q_out, int64_t ld_q_out, int64_t n_tok,
+                          const int32_t* tok_start, const float* cos_sin, int64_t n_pos, void* k_pool, int64_t ld_k,
+                          void* v_pool, int64_t ld_v, float* k_scale, float* v_scale, int64_t n_pages,
+                          const int32_t* page_table, int64_t page_table_stride, const int32_t* ctx_len, int batch,
+                          int32_t* ctx_len_out);
+
+/* Attention of one query per sequence, at position ctx_len[b] - 1, over the cached tokens that it sees:
+ *     S_b = { s < n : k_swa = 0, or s >= n - k_swa, or s < k_sink },  n = ctx_len[b]
+ *     out[b,h,:] = sum_{s in S_b} softmax_s(sm_scale q[b,h].k[s]) v[s],   lse[b,h] = log sum_s exp(logit)
+ * fp32 softmax and accumulation, products in the tensor cores' 16-bit types.  A sequence with n = 0 has out = 0 and lse = -inf.
+ * Nothing outside S_b is read for its value: pages behind the last token, or before the window, may hold anything.
+ *   q, out     [batch, n_heads, d_qk] / [batch, n_heads, d_v] rows of ld_q / ld_out elements per sequence (heads contiguous)
+ *   lse        optional fp32 [batch, n_heads]
+ *   k_pool ... page_table as in lsa_kv_append; ctx_len int32 [batch]: lengths with the new token
+ * The cached tokens of all sequences are dealt evenly to the SMs, and parts of a sequence are joined by their log-sum-exps (in
+ * a fixed order: the same call gives the same bits).  A sequence's rounding depends on the batch that it is dealt with.
+ * A length outside [0, page_table_stride * kv_page] (it is clamped to that range) or a page number outside [0, n_pages) (its tokens count
+ * as zero rows) is reported as LSA_ERR_INDEX by lsa_status; other sequences are not affected. */
+LSA_API int lsa_paged_attn(lsa_ctx* ctx, const lsa_kv_params* p, const void* q, int64_t ld_q, const void* k_pool, int64_t ld_k,
+                           const void* v_pool, int64_t ld_v, const float* k_scale, const float* v_scale, int64_t n_pages,
+                           const int32_t* page_table, int64_t page_table_stride, const int32_t* ctx_len, int batch, void* out,
+                           int64_t ld_out, float* lse);
 
 #ifdef __cplusplus
 }

@@ -381,6 +381,45 @@ def gather_paged(pool_rows, page_table_row, n, kv_page):
     return np.asarray(pool_rows)[paged_rows(np.arange(n), page_table_row, kv_page)]
 
 
+def rotate_pairs(x, cos, sin, at, interleaved):
+    """Position rotation of one head: x [d]; cos, sin [n] of the position's n angles.
+
+    The 2 n dims from `at` on are n pairs, (j, j + n) or (2 j, 2 j + 1); the pair (a, b) becomes
+    (a cos - b sin, b cos + a sin).  The other dims stay.
+    """
+    x = np.array(x, dtype=np.float64)
+    n = len(cos)
+    for j in range(n):
+        i0, i1 = (at + 2 * j, at + 2 * j + 1) if interleaved else (at + j, at + j + n)
+        a, b = x[i0], x[i1]
+        x[i0], x[i1] = a * cos[j] - b * sin[j], b * cos[j] + a * sin[j]
+    return x
+
+
+def seen_tokens(n, sink, window):
+    """Positions that the query at position n - 1 sees: all of 0 .. n - 1, or with a window the last `window` of them and
+    the first `sink`."""
+    s = np.arange(n)
+    return s[(s >= n - window) | (s < sink)] if window > 0 else s
+
+
+def paged_attend(q, k_rows, v_rows, page_table_row, n, kv_page, n_kv_heads, *, sink=0, window=0, sm_scale):
+    """Attention of one query over one sequence's paged cache.
+
+    q [H, d_qk]; k_rows [rows, n_kv_heads, d_qk], v_rows [rows, n_kv_heads, d_v] real values of the pool; query head h
+    reads KV head h // (H / n_kv_heads).  Returns (out [H, d_v], lse [H]); no token seen: zeros and -inf.
+    """
+    H, d_v = q.shape[0], v_rows.shape[-1]
+    pos = seen_tokens(n, sink, window)
+    if len(pos) == 0:
+        return np.zeros((H, d_v)), np.full(H, -np.inf)
+    rows = paged_rows(pos, page_table_row, kv_page)
+    group = H // n_kv_heads
+    parts = [attend(q[g * group:(g + 1) * group], k_rows[rows, g], v_rows[rows, g], np.arange(len(rows)), sm_scale)
+             for g in range(n_kv_heads)]
+    return np.concatenate([p[0] for p in parts]), np.concatenate([p[1] for p in parts])
+
+
 # ----------------------------------------------------------------------------
 # whole path for one query
 # ----------------------------------------------------------------------------

@@ -37,6 +37,12 @@ class LsaParams(ctypes.Structure):
                 ("paged", c_int32), ("kv_page", c_int32), ("pooling", c_int32)]
 
 
+class LsaKvParams(ctypes.Structure):
+    _fields_ = [("struct_size", c_uint32), ("dtype", c_int32), ("cache_e4m3", c_int32), ("latent", c_int32), ("n_heads", c_int32),
+                ("n_kv_heads", c_int32), ("d_qk", c_int32), ("d_v", c_int32), ("kv_page", c_int32), ("d_rope", c_int32),
+                ("rope_at", c_int32), ("rope_interleaved", c_int32), ("k_sink", c_int32), ("k_swa", c_int32), ("sm_scale", c_float)]
+
+
 EXPORTS = {
     "lsa_create": (c_int, [POINTER(c_void_p), c_int, c_void_p, c_void_p, c_size_t]),
     "lsa_destroy": (c_int, [c_void_p]),
@@ -74,6 +80,12 @@ EXPORTS = {
     "lsa_layer_group_host": (c_int, [c_void_p, POINTER(LsaParams), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                                      c_int64, c_int64, c_int64, POINTER(c_void_p), POINTER(c_void_p), POINTER(c_void_p),
                                      c_int64, c_int64, POINTER(c_void_p), c_int64, POINTER(c_void_p), c_size_t]),
+    "lsa_kv_workspace_bytes": (c_int, [POINTER(LsaKvParams), POINTER(c_size_t)]),
+    "lsa_kv_append": (c_int, [c_void_p, POINTER(LsaKvParams), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                              c_int64, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                              c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p]),
+    "lsa_paged_attn": (c_int, [c_void_p, POINTER(LsaKvParams), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                               c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int, c_void_p, c_int64, c_void_p]),
     "lsa_host_stage_bytes": (c_int, [POINTER(LsaParams), c_int64, POINTER(c_size_t)]),
 }
 
@@ -131,6 +143,46 @@ def host_stage_bytes(params: LsaParams, stage_queries: int) -> int:
     return out.value
 
 
+_KV_DTYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
+
+
+def make_kv_params(n_heads: int, n_kv_heads: int, d_qk: int, d_v: int, kv_page: int, latent: bool = False, dtype: str = "bf16",
+                   e4m3: bool = False, d_rope: int = 0, rope_at: int = 0, rope_interleaved: bool = False, sink: int = 0,
+                   window: int = 0, sm_scale: float | None = None) -> LsaKvParams:
+    """lsa_kv_params: a paged key-value cache and the heads that read it.  sm_scale defaults to 1 / sqrt(d_qk)."""
+    return LsaKvParams(ctypes.sizeof(LsaKvParams), tuple(_KV_DTYPES).index(dtype), int(e4m3), int(latent), n_heads, n_kv_heads, d_qk, d_v,
+                       kv_page, d_rope, rope_at, int(rope_interleaved), sink, window, d_qk ** -0.5 if sm_scale is None else sm_scale)
+
+
+def kv_workspace_bytes(kv: LsaKvParams) -> int:
+    out = c_size_t(0)
+    r = lib().lsa_kv_workspace_bytes(ctypes.byref(kv), ctypes.byref(out))
+    if r != 0:
+        raise LsaError(r, "lsa_kv_workspace_bytes")
+    return out.value
+
+
+def _kv_rows(t, width: int, dtype, where: str, rows: int | None = None):
+    """(pointer, elements from one row to the next) of rows of `width` elements, given as [rows, width] or [rows, heads, dims]."""
+    if t is None:
+        return None, 0
+    st, sh = t.stride(), t.shape
+    n = len(sh)
+    inner = n >= 2 and st[-1] == 1 and (n == 2 or (n == 3 and (sh[1] == 1 or st[1] == sh[2])))
+    if not inner or t.dtype != dtype or (sh[1] if n == 2 else sh[1] * sh[2]) != width or (rows is not None and sh[0] != rows):
+        raise LsaError(-1, where, f"rows of {width} {dtype} wanted{'' if rows is None else f', {rows} of them'}: got {tuple(sh)} {t.dtype}, strides {st}")
+    return t.data_ptr(), (st[0] if sh[0] > 1 else max(st[0], width))
+
+
+def _kv_flat(t, dtype, count: int, where: str, exact: bool = True):
+    """Pointer to a contiguous array of `count` elements (or at least as many)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or not t.is_contiguous() or (t.numel() != count if exact else t.numel() < count):
+        raise LsaError(-1, where, f"{count} contiguous {dtype} wanted: got {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
 STATIC_SCRATCH_BYTES = 8 << 20
 
 
@@ -159,10 +211,17 @@ def index_static_status(device, stream=None) -> int:
 class Context:
     """lsa_ctx bound to the current torch CUDA stream; owns its workspace tensor."""
 
-    def __init__(self, params: LsaParams, n_query: int, n_key_max: int, batch: int = 1, device=None, stream=None):
+    def __init__(self, params: LsaParams | None, n_query: int, n_key_max: int, batch: int = 1, device=None, stream=None,
+                 kv: LsaKvParams | None = None):
+        """params: the sparse path's (None: the context serves kv_append and paged_attn only); kv: those calls' parameters."""
         self.params = params
+        self.kv = kv
         self.device = torch.device(device if device is not None else "cuda:0")
-        nbytes = workspace_bytes(params, n_query, n_key_max, batch)
+        nbytes = workspace_bytes(params, n_query, n_key_max, batch) if params is not None or kv is None else 0
+        if kv is not None:
+            nbytes = max(nbytes, kv_workspace_bytes(kv))
+            self._kv_ref = ctypes.byref(kv)
+            self._kv_dtype = tuple(_KV_DTYPES.values())[kv.dtype]
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         h = c_void_p()
@@ -271,3 +330,43 @@ class Context:
                                              _p(k_scale), _p(kmean), q_pos0, n_query, n_key, _parr(q_host), _parr(k),
                                              _parr(v), k[0].stride(0), v[0].stride(0), _parr(out_host), stage_queries,
                                              _parr(stage), stage[0].numel()), "lsa_layer_group_host")
+
+    def _kv_cache(self, k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where):
+        """The arguments of a cache: pools as [rows, heads * dims] or [rows, heads, dims], scales as [rows, heads]."""
+        kv = self.kv
+        if kv is None:
+            raise LsaError(-1, where, "the context was made without kv parameters")
+        rows, batch = k_pool.shape[0], page_table.shape[0]
+        dtype = k_pool.dtype if kv.cache_e4m3 and k_pool.dtype in (torch.uint8, torch.float8_e4m3fn) else torch.uint8 if kv.cache_e4m3 else self._kv_dtype
+        if rows % kv.kv_page:
+            raise LsaError(-1, where, f"a pool of {rows} rows is not a whole number of pages of {kv.kv_page}")
+        if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.stride(1) != 1:
+            raise LsaError(-1, where, "page_table: int32 [batch, pages] with contiguous rows wanted")
+        return (*_kv_rows(k_pool, kv.n_kv_heads * kv.d_qk, dtype, where), *_kv_rows(v_pool, kv.n_kv_heads * kv.d_v, dtype, where, rows),
+                _kv_flat(k_scale, torch.float32, rows * kv.n_kv_heads, where), _kv_flat(v_scale, torch.float32, rows * kv.n_kv_heads, where),
+                rows // kv.kv_page, page_table.data_ptr(), page_table.stride(0) if batch > 1 else page_table.shape[1],
+                _kv_flat(ctx_len, torch.int32, batch, where), batch)
+
+    def kv_append(self, k_new, v_new, k_pool, v_pool, page_table, ctx_len, ctx_len_out=None, tok_start=None, q=None, q_out=None,
+                  cos_sin=None, k_scale=None, v_scale=None):
+        """lsa_kv_append: new tokens [n_tok, heads, dims] into the cache, rotated; q (optional) rotated into q_out."""
+        cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, "lsa_kv_append")
+        kv, batch = self.kv, cache[-1]
+        n_tok = k_new.shape[0]
+        if cos_sin is not None and (cos_sin.dim() != 2 or cos_sin.shape[1] != kv.d_rope):
+            raise LsaError(-1, "lsa_kv_append", f"cos_sin: [positions, {kv.d_rope}] wanted, got {tuple(cos_sin.shape)}")
+        self._chk(lib().lsa_kv_append(
+            self.h, self._kv_ref, *_kv_rows(k_new, kv.n_kv_heads * kv.d_qk, self._kv_dtype, "k_new"),
+            *_kv_rows(v_new, kv.n_kv_heads * kv.d_v, self._kv_dtype, "v_new", n_tok),
+            *_kv_rows(q, kv.n_heads * kv.d_qk, self._kv_dtype, "q", n_tok), *_kv_rows(q_out, kv.n_heads * kv.d_qk, self._kv_dtype, "q_out", n_tok),
+            n_tok, _kv_flat(tok_start, torch.int32, batch + 1, "tok_start"),
+            _kv_flat(cos_sin, torch.float32, 0 if cos_sin is None else cos_sin.numel(), "cos_sin"), 0 if cos_sin is None else cos_sin.shape[0],
+            *cache, _kv_flat(ctx_len_out, torch.int32, batch, "ctx_len_out")), "lsa_kv_append")
+
+    def paged_attn(self, q, k_pool, v_pool, page_table, ctx_len, out, lse=None, k_scale=None, v_scale=None):
+        """lsa_paged_attn: q [batch, heads, d_qk] over each sequence's cached tokens -> out [batch, heads, d_v], lse [batch, heads]."""
+        cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, "lsa_paged_attn")
+        kv, batch = self.kv, cache[-1]
+        out_ptr, ld_out = _kv_rows(out, kv.n_heads * kv.d_v, self._kv_dtype, "out", batch)
+        self._chk(lib().lsa_paged_attn(self.h, self._kv_ref, *_kv_rows(q, kv.n_heads * kv.d_qk, self._kv_dtype, "q", batch), *cache, out_ptr, ld_out,
+                                       _kv_flat(lse, torch.float32, batch * kv.n_heads, "lse")), "lsa_paged_attn")

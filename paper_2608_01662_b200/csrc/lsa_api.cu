@@ -176,6 +176,32 @@ WsLayout ws_layout(const lsa_params* p, int64_t n_query, int64_t n_key_max, int 
 }
 
 int* status_word(lsa_ctx* c) { return c->ws ? reinterpret_cast<int*>(c->ws) : nullptr; }
+// A second word for numbers of the caller's that point outside their arrays: waits end when the status word is raised, and one
+// sequence's bad page must not end those of the others.
+int* notice_word(lsa_ctx* c) { return c->ws ? reinterpret_cast<int*>(c->ws) + 1 : nullptr; }
+
+// The context's device for the time of a call; the caller's is current again afterwards.
+class OnDevice {
+ public:
+  explicit OnDevice(int device) {
+    e_ = cudaGetDevice(&before_);
+    if (e_ == cudaSuccess && before_ != device) {
+      e_ = cudaSetDevice(device);
+      moved_ = e_ == cudaSuccess;
+    }
+  }
+  ~OnDevice() {
+    if (moved_) (void)cudaSetDevice(before_);
+  }
+  OnDevice(const OnDevice&) = delete;
+  OnDevice& operator=(const OnDevice&) = delete;
+  cudaError_t error() const { return e_; }
+
+ private:
+  int before_ = 0;
+  bool moved_ = false;
+  cudaError_t e_;
+};
 
 // Number of row splits per sequence in paged (decode) attention, and (tcgen05 kernel) the parts, 2^v_shift, that the value dims
 // of a split are taken in by clusters of their own.  Blocks run one per SM in waves; a block costs its share of the 64-key tiles
@@ -462,9 +488,11 @@ int lsa_status(lsa_ctx* c, int* device_status) {
   cudaError_t e = cudaStreamSynchronize(c->stream);
   if (e != cudaSuccess) return cuda_fail(c, e);
   if (c->ws == nullptr) return LSA_OK;
-  e = cudaMemcpyAsync(device_status, c->ws, sizeof(int), cudaMemcpyDeviceToHost, c->stream);
-  if (e == cudaSuccess) e = cudaMemsetAsync(c->ws, 0, sizeof(int), c->stream);
+  int words[2] = {0, 0};   // the status word, the notice word
+  e = cudaMemcpyAsync(words, c->ws, sizeof(words), cudaMemcpyDeviceToHost, c->stream);
+  if (e == cudaSuccess) e = cudaMemsetAsync(c->ws, 0, sizeof(words), c->stream);
   if (e == cudaSuccess) e = cudaStreamSynchronize(c->stream);
+  *device_status = words[0] != 0 ? words[0] : words[1];
   return e == cudaSuccess ? LSA_OK : cuda_fail(c, e);
 }
 
@@ -484,7 +512,7 @@ const char* lsa_strerror(int err) {
     case LSA_ERR_CUDA: return "CUDA runtime error";
     case LSA_ERR_TIMEOUT: return "device-side wait timed out";
     case LSA_ERR_CAPACITY: return "request exceeds the fixed scratch capacity of this entry point";
-    case LSA_ERR_INDEX: return "cache row number outside the cache (checking build)";
+    case LSA_ERR_INDEX: return "cache row, page or position outside its array";
     default: return "unknown error";
   }
 }
@@ -809,6 +837,147 @@ int lsa_layer_group_host(lsa_ctx* c, const lsa_params* p, const void* q_idx_host
   if (ej == cudaSuccess) ej = cudaStreamWaitEvent(c->stream, c->ev_start, 0);
   if (e == cudaSuccess) e = ej;
   if (r != LSA_OK) return r;
+  return e == cudaSuccess ? LSA_OK : cuda_fail(c, e);
+}
+
+// ---- paged key-value caches without an indexer
+
+static int check_kv_params(const lsa_kv_params* p) {
+  if (p == nullptr || p->struct_size != sizeof(lsa_kv_params)) return LSA_ERR_ARG;
+  if (p->dtype != LSA_DTYPE_BF16 && p->dtype != LSA_DTYPE_FP16) return LSA_ERR_ARG;
+  for (const int32_t flag : {p->cache_e4m3, p->latent, p->rope_interleaved})
+    if (flag != 0 && flag != 1) return LSA_ERR_ARG;
+  if (p->n_heads <= 0 || p->n_kv_heads <= 0 || p->n_heads % p->n_kv_heads != 0) return LSA_ERR_ARG;
+  if (p->k_sink < 0 || p->k_swa < 0 || p->d_rope < 0 || p->rope_at < 0) return LSA_ERR_ARG;
+  if (!(p->sm_scale > 0.f) || !(p->sm_scale < 3e38f)) return LSA_ERR_ARG;
+  if (p->latent) {
+    if (p->n_kv_heads != 1 || p->n_heads > 64 || p->d_qk != 576 || p->d_v != 512 || p->cache_e4m3) return LSA_ERR_SHAPE;
+    if (p->kv_page != 64 && p->kv_page != 128 && p->kv_page != 256) return LSA_ERR_SHAPE;
+  } else {
+    if ((p->d_qk != 64 && p->d_qk != 128) || p->d_v != p->d_qk) return LSA_ERR_SHAPE;
+    if (p->n_heads / p->n_kv_heads > 16 || p->n_heads > 4096) return LSA_ERR_SHAPE;
+    if (!pow2(p->kv_page) || p->kv_page < 16 || p->kv_page > 256) return LSA_ERR_SHAPE;
+  }
+  if (p->d_rope % 16 != 0 || p->rope_at % 16 != 0 || p->rope_at > p->d_qk || p->d_rope > p->d_qk - p->rope_at) return LSA_ERR_SHAPE;
+  return LSA_OK;
+}
+
+// The cache as both calls take it.
+static int check_kv_cache(const lsa_kv_params* p, const void* k_pool, int64_t ld_k, const void* v_pool, int64_t ld_v, const float* k_scale,
+                          const float* v_scale, int64_t n_pages, const int32_t* page_table, int64_t page_table_stride,
+                          const int32_t* ctx_len, int batch) {
+  if (batch < 0 || n_pages < 0 || page_table_stride <= 0) return LSA_ERR_ARG;
+  if (batch > 0 && (k_pool == nullptr || page_table == nullptr || ctx_len == nullptr)) return LSA_ERR_ARG;
+  if (batch > 0 && (v_pool == nullptr) != (p->latent != 0)) return LSA_ERR_ARG;
+  if ((k_scale != nullptr) != (p->cache_e4m3 != 0) || (v_scale != nullptr) != (p->cache_e4m3 != 0)) return LSA_ERR_ARG;
+  const int64_t unit = p->cache_e4m3 ? 16 : 8;   // elements of 16 bytes
+  if (ld_k < static_cast<int64_t>(p->n_kv_heads) * p->d_qk || ld_k % unit != 0 || !aligned16(k_pool)) return LSA_ERR_SHAPE;
+  if (!p->latent && (ld_v < static_cast<int64_t>(p->n_kv_heads) * p->d_v || ld_v % unit != 0 || !aligned16(v_pool))) return LSA_ERR_SHAPE;
+  if (ld_k > (1ll << 31) || (!p->latent && ld_v > (1ll << 31))) return LSA_ERR_SHAPE;
+  // rows and positions are 32-bit numbers in the kernels
+  constexpr int64_t kMost = (1ll << 31) - 1024;
+  if (n_pages > kMost / p->kv_page || page_table_stride > kMost / p->kv_page) return LSA_ERR_SHAPE;
+  return LSA_OK;
+}
+
+static int log2_of(int x) {
+  int s = 0;
+  while ((1 << s) < x) ++s;
+  return s;
+}
+
+struct KvScratch {
+  size_t part_out, part_lse, total;
+};
+static KvScratch kv_scratch(const lsa_kv_params* p) {
+  const size_t rows = 2 * static_cast<size_t>(lsa::kMaxPagedUnits) * lsa::paged_rows(p->latent, p->n_heads, p->n_kv_heads);
+  KvScratch s{};
+  s.part_out = kStatusBytes;
+  s.part_lse = s.part_out + align_up(rows * p->d_v * sizeof(float), 256);
+  s.total = s.part_lse + align_up(rows * sizeof(float), 256);
+  return s;
+}
+
+int lsa_kv_workspace_bytes(const lsa_kv_params* p, size_t* bytes) {
+  if (bytes == nullptr) return LSA_ERR_ARG;
+  const int r = check_kv_params(p);
+  if (r != LSA_OK) return r;
+  *bytes = kv_scratch(p).total;
+  return LSA_OK;
+}
+
+int lsa_kv_append(lsa_ctx* c, const lsa_kv_params* p, const void* k_new, int64_t ld_k_new, const void* v_new, int64_t ld_v_new,
+                  const void* q, int64_t ld_q, void* q_out, int64_t ld_q_out, int64_t n_tok, const int32_t* tok_start,
+                  const float* cos_sin, int64_t n_pos, void* k_pool, int64_t ld_k, void* v_pool, int64_t ld_v, float* k_scale,
+                  float* v_scale, int64_t n_pages, const int32_t* page_table, int64_t page_table_stride, const int32_t* ctx_len,
+                  int batch, int32_t* ctx_len_out) {
+  int r = check_kv_params(p);
+  if (r != LSA_OK) return r;
+  r = check_kv_cache(p, k_pool, ld_k, v_pool, ld_v, k_scale, v_scale, n_pages, page_table, page_table_stride, ctx_len, batch);
+  if (r != LSA_OK) return r;
+  if (n_tok < 0 || n_tok > 0x7fffffff || n_pos < 0 || (tok_start == nullptr && n_tok != batch)) return LSA_ERR_ARG;
+  if ((q == nullptr) != (q_out == nullptr) || (cos_sin == nullptr) != (p->d_rope == 0)) return LSA_ERR_ARG;
+  if (n_tok > 0 && (k_new == nullptr || (v_new == nullptr) != (p->latent != 0))) return LSA_ERR_ARG;
+  const int64_t wk = static_cast<int64_t>(p->n_kv_heads) * p->d_qk, wq = static_cast<int64_t>(p->n_heads) * p->d_qk;
+  auto rows_ok = [](const void* x, int64_t ld, int64_t width) { return x == nullptr || (aligned16(x) && ld >= width && ld % 8 == 0 && ld <= (1ll << 31)); };
+  if (!rows_ok(k_new, ld_k_new, wk) || !rows_ok(v_new, ld_v_new, wk) || !rows_ok(q, ld_q, wq) || !rows_ok(q_out, ld_q_out, wq)) return LSA_ERR_SHAPE;
+  if (q != nullptr && q == q_out && ld_q != ld_q_out) return LSA_ERR_ARG;
+  if (cos_sin != nullptr && !aligned16(cos_sin)) return LSA_ERR_SHAPE;
+  if (c == nullptr) return LSA_ERR_ARG;   // (last: the arguments are judged without a device)
+  if (batch == 0) return LSA_OK;
+  if (n_tok == 0 && ctx_len_out == nullptr) return LSA_OK;
+  const OnDevice device(c->device);
+  if (device.error() != cudaSuccess) return cuda_fail(c, device.error());
+  lsa::KvAppendArgs a{};
+  a.fp16 = p->dtype == LSA_DTYPE_FP16; a.e4m3 = p->cache_e4m3; a.latent = p->latent;
+  a.H = p->n_heads; a.G = p->n_kv_heads; a.d = p->d_qk; a.dv = p->d_v;
+  a.d_rope = p->d_rope; a.rope_at = p->rope_at; a.interleaved = p->rope_interleaved;
+  a.page_shift = log2_of(p->kv_page); a.batch = batch;
+  a.n_tok = n_tok; a.n_pos = n_pos; a.n_pages = n_pages; a.pt_stride = page_table_stride;
+  a.ld_k_new = ld_k_new; a.ld_v_new = ld_v_new; a.ld_q = ld_q; a.ld_q_out = ld_q_out; a.ld_k = ld_k; a.ld_v = ld_v;
+  a.k_new = k_new; a.v_new = v_new; a.q = q; a.q_out = q_out;
+  a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;
+  a.tok_start = tok_start; a.cos_sin = cos_sin; a.page_table = page_table; a.ctx_len = ctx_len; a.ctx_len_out = ctx_len_out;
+  a.notice = notice_word(c); a.sm_count = c->sm_count;
+  const cudaError_t e = timed(c, LSA_K_MEANS, [&] { return lsa::launch_kv_append(a, c->stream, &c->launches); });
+  return e == cudaSuccess ? LSA_OK : cuda_fail(c, e);
+}
+
+int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld_q, const void* k_pool, int64_t ld_k,
+                   const void* v_pool, int64_t ld_v, const float* k_scale, const float* v_scale, int64_t n_pages,
+                   const int32_t* page_table, int64_t page_table_stride, const int32_t* ctx_len, int batch, void* out,
+                   int64_t ld_out, float* lse) {
+  int r = check_kv_params(p);
+  if (r != LSA_OK) return r;
+  r = check_kv_cache(p, k_pool, ld_k, v_pool, ld_v, k_scale, v_scale, n_pages, page_table, page_table_stride, ctx_len, batch);
+  if (r != LSA_OK) return r;
+  if (batch > 0 && (q == nullptr || out == nullptr)) return LSA_ERR_ARG;
+  if (!aligned16(q) || !aligned16(out) || ld_q % 8 != 0 || ld_out % 8 != 0) return LSA_ERR_SHAPE;
+  if (ld_q < static_cast<int64_t>(p->n_heads) * p->d_qk || ld_out < static_cast<int64_t>(p->n_heads) * p->d_v) return LSA_ERR_SHAPE;
+  if (c == nullptr) return LSA_ERR_ARG;
+  if (batch == 0) return LSA_OK;
+  const KvScratch s = kv_scratch(p);
+  if (c->ws == nullptr || s.total > c->ws_bytes) return LSA_ERR_WORKSPACE;
+  const OnDevice device(c->device);
+  if (device.error() != cudaSuccess) return cuda_fail(c, device.error());
+  lsa::PagedAttnArgs a{};
+  a.fp16 = p->dtype == LSA_DTYPE_FP16; a.e4m3 = p->cache_e4m3; a.latent = p->latent;
+  a.H = p->n_heads; a.G = p->n_kv_heads; a.d = p->d_qk; a.dv = p->d_v;
+  a.sink = p->k_sink; a.window = p->k_swa; a.page_shift = log2_of(p->kv_page); a.batch = batch;
+  a.max_len = static_cast<int>(page_table_stride * p->kv_page); a.n_pages = static_cast<int>(n_pages);
+  a.units = c->sm_count < lsa::kMaxPagedUnits ? c->sm_count : lsa::kMaxPagedUnits;
+  a.min_tiles = 1;
+  a.pt_stride = page_table_stride; a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out;
+  a.scale2 = p->sm_scale * 1.4426950408889634f;
+  a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;
+  a.page_table = page_table; a.ctx_len = ctx_len; a.out = out; a.lse = lse;
+  a.part_out = reinterpret_cast<float*>(c->ws + s.part_out);
+  a.part_lse = reinterpret_cast<float*>(c->ws + s.part_lse);
+  a.status = status_word(c); a.notice = notice_word(c);
+  c->last_attn_rows = nullptr;   // (the launch before the next sparse one is no longer one on its row lists)
+  const cudaError_t e = timed(c, LSA_K_ATTN, [&] {
+    return p->latent ? lsa::launch_paged_attn_tc(a, c->stream, &c->launches) : lsa::launch_paged_attn(a, c->stream, &c->launches);
+  });
   return e == cudaSuccess ? LSA_OK : cuda_fail(c, e);
 }
 

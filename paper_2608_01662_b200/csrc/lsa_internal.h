@@ -222,6 +222,54 @@ struct MergeArgs {
 };
 cudaError_t launch_merge_parts(const MergeArgs& a, cudaStream_t st, int64_t* n_launch);
 
+// ---- paged key-value caches (lsa_kv_append, lsa_paged_attn)
+struct KvAppendArgs {
+  int fp16, e4m3, latent, H, G, d, dv;   // element type, heads, dims of a query or key head and of a value head
+  int d_rope, rope_at, interleaved;
+  int page_shift, batch;
+  int64_t n_tok, n_pos, n_pages, pt_stride;
+  int64_t ld_k_new, ld_v_new, ld_q, ld_q_out, ld_k, ld_v;
+  const void *k_new, *v_new, *q;
+  void *q_out, *k_pool, *v_pool;
+  float *k_scale, *v_scale;
+  const int32_t* tok_start;
+  const float* cos_sin;
+  const int32_t* page_table;
+  const int32_t* ctx_len;
+  int32_t* ctx_len_out;
+  int* notice;
+  int sm_count;
+};
+cudaError_t launch_kv_append(const KvAppendArgs& a, cudaStream_t st, int64_t* n_launch);
+
+struct PagedAttnArgs {
+  int fp16, e4m3, latent, H, G, d, dv;
+  int sink, window, page_shift, batch;
+  int max_len;                // tokens that a row of the page table covers
+  int n_pages;
+  int units;                  // blocks that the list of tiles is dealt to
+  int min_tiles;              // entries of a unit at least
+  int64_t pt_stride, ld_q, ld_k, ld_v, ld_out;
+  float scale2;               // sm_scale * log2(e)
+  const void *q, *k_pool, *v_pool;
+  const float *k_scale, *v_scale;
+  const int32_t* page_table;
+  const int32_t* ctx_len;
+  void* out;
+  float* lse;
+  float* part_out;            // fp32 [2 * units][rows of a unit][dv], normalised
+  float* part_lse;            // fp32 [2 * units][rows of a unit], log2
+  int* status;
+  int* notice;
+};
+constexpr int kMaxPagedUnits = 160;     // one block per SM: the scratch is sized for that many
+// query heads that a unit works on at a time (rows of its partial results)
+int paged_rows(int latent, int H, int G);
+cudaError_t launch_paged_attn(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch);      // separate keys and values
+cudaError_t launch_paged_attn_tc(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch);   // latent rows
+// joins the parts that units of the two kernels above left; shift, blocks: keys of a tile (log2), blocks of KV heads of its list
+cudaError_t launch_paged_join(const PagedAttnArgs& a, int shift, int blocks, cudaStream_t st, int64_t* n_launch);
+
 // One block waits on an mbarrier nobody arrives on, for at most budget_cycles (thread 0) before the status word gets
 // the time-out code; *waited_ok (optional, zeroed by the caller) counts threads whose wait claimed success.
 cudaError_t launch_selftest_wait(int* status, long long budget_cycles, int* waited_ok, cudaStream_t st, int64_t* n_launch);
