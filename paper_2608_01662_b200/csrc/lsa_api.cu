@@ -887,14 +887,15 @@ static int log2_of(int x) {
 }
 
 struct KvScratch {
-  size_t part_out, part_lse, total;
+  size_t part_out, part_lse, parts, total;
 };
 static KvScratch kv_scratch(const lsa_kv_params* p) {
   const size_t rows = 2 * static_cast<size_t>(lsa::kMaxPagedUnits) * lsa::paged_rows(p->latent, p->n_heads, p->n_kv_heads);
   KvScratch s{};
   s.part_out = kStatusBytes;
   s.part_lse = s.part_out + align_up(rows * p->d_v * sizeof(float), 256);
-  s.total = s.part_lse + align_up(rows * sizeof(float), 256);
+  s.parts = s.part_lse + align_up(rows * sizeof(float), 256);
+  s.total = s.parts + align_up(lsa::kMaxPagedUnits * sizeof(int4), 256);
   return s;
 }
 
@@ -971,8 +972,10 @@ int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld
   a.scale2 = p->sm_scale * 1.4426950408889634f;
   a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;
   a.page_table = page_table; a.ctx_len = ctx_len; a.out = out; a.lse = lse;
+  if (lsa::paged_entries(a) >= (1ll << 31) - a.units) return LSA_ERR_SHAPE;   // (2^35 tokens and more)
   a.part_out = reinterpret_cast<float*>(c->ws + s.part_out);
   a.part_lse = reinterpret_cast<float*>(c->ws + s.part_lse);
+  a.parts = reinterpret_cast<int4*>(c->ws + s.parts);
   a.status = status_word(c); a.notice = notice_word(c);
   c->last_attn_rows = nullptr;   // (the launch before the next sparse one is no longer one on its row lists)
   const cudaError_t e = timed(c, LSA_K_ATTN, [&] {

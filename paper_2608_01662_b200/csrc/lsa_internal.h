@@ -257,18 +257,20 @@ struct PagedAttnArgs {
   const int32_t* ctx_len;
   void* out;
   float* lse;
-  float* part_out;            // fp32 [2 * units][rows of a unit][dv], normalised
+  float* part_out;            // fp32 [2 * units][rows of a unit][dv] (latent: [dv][64 heads]), normalised
   float* part_lse;            // fp32 [2 * units][rows of a unit], log2
+  int4* parts;                // [units]: what there is to join
   int* status;
   int* notice;
 };
 constexpr int kMaxPagedUnits = 160;     // one block per SM: the scratch is sized for that many
 // query heads that a unit works on at a time (rows of its partial results)
 int paged_rows(int latent, int H, int G);
+// entries of the list at most: tiles of `batch` sequences of max_len tokens, times the blocks of KV heads
+int64_t paged_entries(const PagedAttnArgs& a);
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch);      // separate keys and values
 cudaError_t launch_paged_attn_tc(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch);   // latent rows
-// joins the parts that units of the two kernels above left; shift, blocks: keys of a tile (log2), blocks of KV heads of its list
-cudaError_t launch_paged_join(const PagedAttnArgs& a, int shift, int blocks, cudaStream_t st, int64_t* n_launch);
+
 
 // One block waits on an mbarrier nobody arrives on, for at most budget_cycles (thread 0) before the status word gets
 // the time-out code; *waited_ok (optional, zeroed by the caller) counts threads whose wait claimed success.

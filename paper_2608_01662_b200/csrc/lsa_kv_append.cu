@@ -71,7 +71,7 @@ constexpr int kRowsInFlight = 4;
 template <int D>
 constexpr int kFewTokens = D == 576 ? 576 : 512;
 template <int D>
-constexpr int kManyTokens = D == 576 ? 288 : 256;
+constexpr int kManyTokens = D == 576 ? 288 : 64;
 
 // D: dims of a query or key head (and of a value head, if there are any).  Blocks are a multiple of 32 and of D / 16 threads.
 template <typename T, int D, bool kE4M3>
@@ -79,8 +79,38 @@ __global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a
   constexpr int kPlaces = D / 16;   // threads of a row
   const int tid = threadIdx.x;
   const int64_t tok = blockIdx.x;
+  // ---- the thread's place: vectors v0 and v1 (of eight elements) of every row it visits
+  const int place = tid % kPlaces, lane_row = tid / kPlaces, rows_at_once = blockDim.x / kPlaces;
+  const bool turns = 16 * place < a.d_rope;
+  int v0, v1;
+  if (turns) {
+    v0 = a.rope_at / 8 + (a.interleaved ? 2 * place : place);
+    v1 = v0 + (a.interleaved ? 1 : a.d_rope / 16);
+  } else {   // two neighbours of what is left (it starts and ends on a multiple of 16 dims)
+    v0 = 2 * place - a.d_rope / 8;
+    if (v0 >= a.rope_at / 8) v0 += a.d_rope / 8;
+    v1 = v0 + 1;
+  }
+  // rows of the token: query heads, key heads, value heads
+  const int n_q = a.q != nullptr ? a.H : 0, n_k = n_q + a.G, n_rows = a.latent ? n_k : n_k + a.G;
+  const bool in_place = a.q == a.q_out;
+  auto skipped = [&](int r) { return r >= n_rows || (r < n_q && in_place && !turns); };   // (what is not rotated in place stays)
+  uint4 u[kRowsInFlight][2];
+  auto fetch = [&](int r0) {
+#pragma unroll
+    for (int k = 0; k < kRowsInFlight; ++k) {
+      const int r = r0 + k * rows_at_once + lane_row;
+      if (skipped(r)) continue;
+      const T* src = r < n_q ? static_cast<const T*>(a.q) + tok * a.ld_q + r * D
+                     : r < n_k ? static_cast<const T*>(a.k_new) + tok * a.ld_k_new + (r - n_q) * D
+                               : static_cast<const T*>(a.v_new) + tok * a.ld_v_new + (r - n_k) * D;
+      u[k][0] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * v0));
+      u[k][1] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * v1));
+    }
+  };
   pdl_wait();
   pdl_launch_dependents();
+  fetch(0);   // the rows do not depend on where they go: they are on their way while that is looked up
 
   // ---- the token's sequence, position and cache row (the same loads in every thread of the block)
   int b = static_cast<int>(tok);
@@ -111,14 +141,8 @@ __global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a
   if (mine && !fits && tid == 0) paged::report_index(a.notice);
 
   if (fits) {
-    // ---- the thread's place: vectors v0 and v1 (of eight elements) of every row it visits
-    const int place = tid % kPlaces, lane_row = tid / kPlaces, rows_at_once = blockDim.x / kPlaces;
-    const bool turns = 16 * place < a.d_rope;
-    int v0, v1;
     float c[8], s[8];
     if (turns) {
-      v0 = a.rope_at / 8 + (a.interleaved ? 2 * place : place);
-      v1 = v0 + (a.interleaved ? 1 : a.d_rope / 16);
       const float4* cs = reinterpret_cast<const float4*>(a.cos_sin + pos * a.d_rope + 8 * place);
       const float4* sn = reinterpret_cast<const float4*>(a.cos_sin + pos * a.d_rope + a.d_rope / 2 + 8 * place);
 #pragma unroll
@@ -127,15 +151,11 @@ __global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a
         c[4 * h] = x.x; c[4 * h + 1] = x.y; c[4 * h + 2] = x.z; c[4 * h + 3] = x.w;
         s[4 * h] = y.x; s[4 * h + 1] = y.y; s[4 * h + 2] = y.z; s[4 * h + 3] = y.w;
       }
-    } else {   // two neighbours of what is left (it starts and ends on a multiple of 16 dims)
-      v0 = 2 * place - a.d_rope / 8;
-      if (v0 >= a.rope_at / 8) v0 += a.d_rope / 8;
-      v1 = v0 + 1;
+    } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) c[j] = 1.f, s[j] = 0.f;
     }
     auto turn = [&](float (&x)[16]) {
-      if (!turns) return;
       if (a.interleaved) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -152,80 +172,45 @@ __global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a
         }
       }
     };
-
-    // ---- query heads
-    if (a.q != nullptr) {
-      const T* src = static_cast<const T*>(a.q) + tok * a.ld_q;
-      T* dst = static_cast<T*>(a.q_out) + tok * a.ld_q_out;
-      const bool copies = turns || a.q != a.q_out;   // in place: what is not rotated stays
-      for (int r0 = lane_row; copies && r0 < a.H; r0 += kRowsInFlight * rows_at_once) {
-        uint4 u[kRowsInFlight][2];
+    for (int r0 = 0; r0 < n_rows; r0 += kRowsInFlight * rows_at_once) {   // (the same trips for all lanes of a warp: the shuffles below)
+      if (r0 > 0) fetch(r0);
 #pragma unroll
-        for (int k = 0; k < kRowsInFlight; ++k) {
-          const int r = r0 + k * rows_at_once;
-          if (r < a.H) {
-            u[k][0] = *reinterpret_cast<const uint4*>(src + r * D + 8 * v0);
-            u[k][1] = *reinterpret_cast<const uint4*>(src + r * D + 8 * v1);
+      for (int k = 0; k < kRowsInFlight; ++k) {
+        const int r = r0 + k * rows_at_once + lane_row;
+        const bool on = !skipped(r), is_q = r < n_q, is_v = r >= n_k;
+        float x[16];
+        if (turns || kE4M3) {
+          unpack8<T>(u[k][0], x);
+          unpack8<T>(u[k][1], x + 8);
+          if (turns && !is_v) turn(x);
+        }
+        if (kE4M3 && r0 + (k + 1) * rows_at_once > n_q) {   // block-uniform: rows of the cache are among these
+          float top = 0.f;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(x[j]));
+#pragma unroll
+          for (int o = kPlaces / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          if (on && !is_q) {
+            float scale = __fdiv_rn(top, 448.f);
+            if (scale == 0.f) scale = 1.f;   // (a zero row, or one so small that the quotient is)
+            const int g = is_v ? r - n_k : r - n_q;
+            uint8_t* dst = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + row * (is_v ? a.ld_v : a.ld_k) + g * D;
+            *reinterpret_cast<uint2*>(dst + 8 * v0) = codes8(x, scale);
+            *reinterpret_cast<uint2*>(dst + 8 * v1) = codes8(x + 8, scale);
+            if (place == 0) (is_v ? a.v_scale : a.k_scale)[row * a.G + g] = scale;
           }
         }
-#pragma unroll
-        for (int k = 0; k < kRowsInFlight; ++k) {
-          const int r = r0 + k * rows_at_once;
-          if (r < a.H) {
-            if (turns) {
-              float x[16];
-              unpack8<T>(u[k][0], x);
-              unpack8<T>(u[k][1], x + 8);
-              turn(x);
-              u[k][0] = pack8<T>(x);
-              u[k][1] = pack8<T>(x + 8);
-            }
-            *reinterpret_cast<uint4*>(dst + r * D + 8 * v0) = u[k][0];
-            *reinterpret_cast<uint4*>(dst + r * D + 8 * v1) = u[k][1];
+        if (on && (is_q || !kE4M3)) {
+          if (turns && !is_v) {
+            u[k][0] = pack8<T>(x);
+            u[k][1] = pack8<T>(x + 8);
           }
+          T* dst = is_q ? static_cast<T*>(a.q_out) + tok * a.ld_q_out + r * D
+                   : is_v ? static_cast<T*>(a.v_pool) + row * a.ld_v + (r - n_k) * D
+                          : static_cast<T*>(a.k_pool) + row * a.ld_k + (r - n_q) * D;
+          *reinterpret_cast<uint4*>(dst + 8 * v0) = u[k][0];
+          *reinterpret_cast<uint4*>(dst + 8 * v1) = u[k][1];
         }
-      }
-    }
-
-    // ---- key heads, then value heads
-    const int n_rows = a.latent ? a.G : 2 * a.G;
-    for (int r0 = 0; r0 < n_rows; r0 += rows_at_once) {   // (the same trips for all lanes of a warp: the shuffles below)
-      const int r = r0 + lane_row;
-      const bool on = r < n_rows, is_v = r >= a.G;
-      const int g = is_v ? r - a.G : r;
-      uint4 u0 = make_uint4(0, 0, 0, 0), u1 = u0;
-      if (on) {
-        const T* src = is_v ? static_cast<const T*>(a.v_new) + tok * a.ld_v_new + g * D : static_cast<const T*>(a.k_new) + tok * a.ld_k_new + g * D;
-        u0 = *reinterpret_cast<const uint4*>(src + 8 * v0);
-        u1 = *reinterpret_cast<const uint4*>(src + 8 * v1);
-      }
-      float x[16];
-      unpack8<T>(u0, x);
-      unpack8<T>(u1, x + 8);
-      if (!is_v) turn(x);
-      const int64_t at = row * (is_v ? a.ld_v : a.ld_k) + g * D;
-      if constexpr (kE4M3) {
-        float top = 0.f;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(x[j]));
-#pragma unroll
-        for (int o = kPlaces / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        float scale = __fdiv_rn(top, 448.f);
-        if (scale == 0.f) scale = 1.f;   // (a zero row, or one so small that the quotient is)
-        if (on) {
-          uint8_t* dst = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + at;
-          *reinterpret_cast<uint2*>(dst + 8 * v0) = codes8(x, scale);
-          *reinterpret_cast<uint2*>(dst + 8 * v1) = codes8(x + 8, scale);
-          if (place == 0) (is_v ? a.v_scale : a.k_scale)[row * a.G + g] = scale;
-        }
-      } else if (on) {
-        if (turns && !is_v) {
-          u0 = pack8<T>(x);
-          u1 = pack8<T>(x + 8);
-        }
-        T* dst = static_cast<T*>(is_v ? a.v_pool : a.k_pool) + at;
-        *reinterpret_cast<uint4*>(dst + 8 * v0) = u0;
-        *reinterpret_cast<uint4*>(dst + 8 * v1) = u1;
       }
     }
   }

@@ -60,58 +60,48 @@ __device__ __forceinline__ SeqTiles seq_tiles(const PagedAttnArgs& a, int b, int
   return t;
 }
 
-// The list: its length, the entries of a unit, and how many entries lie before sequence b.
-struct List {
-  int64_t total, per;
-};
-// By a whole warp.  `before` (optional): entries of the sequences below b_before.
-__device__ __forceinline__ int64_t warp_sum(int64_t v) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  return v;
-}
-__device__ __forceinline__ List list_of(int64_t total, const PagedAttnArgs& a) {
-  const int64_t even = (total + a.units - 1) / a.units;
-  return {total, even > a.min_tiles ? even : a.min_tiles};
-}
-
-// Where a unit's entries begin.
+// Where a unit is in the list.
 struct Cursor {
   int b, block, tile;   // sequence, block of KV heads, tile
-  int64_t left;         // entries of the unit from here on
+  int left;             // entries of the unit from here on
+  int per;              // entries of every unit but the last
   SeqTiles st;
 };
-// By a whole warp: unit u's first entry.  Each lane counts a run of consecutive sequences.
+// By a whole warp: unit u's first entry.  Each lane counts a run of consecutive sequences.  (The list has fewer than 2^31
+// entries: the host sees to that.)
 __device__ __forceinline__ Cursor first_entry(const PagedAttnArgs& a, int unit, int shift, int blocks, int lane) {
   const int run = (a.batch + 31) / 32;
-  int64_t mine = 0;
+  int mine = 0;
   for (int i = 0; i < run; ++i) {
     const int b = lane * run + i;
     if (b < a.batch) mine += seq_tiles(a, b, shift).count;
   }
-  int64_t upto = mine;   // inclusive scan
+  mine *= blocks;
+  int upto = mine;   // inclusive scan
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+    const int x = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += x;
   }
-  const List l = list_of(__shfl_sync(0xffffffffu, upto, 31) * blocks, a);
+  const int total = __shfl_sync(0xffffffffu, upto, 31);
   Cursor c{};
-  const int64_t t0 = unit * l.per;
-  if (t0 >= l.total) return c;
-  c.left = min64(l.per, l.total - t0);
-  const unsigned past = __ballot_sync(0xffffffffu, upto * blocks > t0);
-  const int owner = __ffs(past) - 1;
-  int64_t base = __shfl_sync(0xffffffffu, upto - mine, owner) * blocks;
+  c.per = max((total - 1) / a.units + 1, a.min_tiles);
+  const int64_t t0 = static_cast<int64_t>(unit) * c.per;
+  if (t0 >= total) return c;
+  c.left = min(c.per, total - static_cast<int>(t0));
+  const int owner = __ffs(__ballot_sync(0xffffffffu, upto > t0)) - 1;
+  int off = static_cast<int>(t0) - __shfl_sync(0xffffffffu, upto - mine, owner);
   c.b = owner * run;
   c.st = seq_tiles(a, c.b, shift);
-  while (base + static_cast<int64_t>(c.st.count) * blocks <= t0) {
-    base += static_cast<int64_t>(c.st.count) * blocks;
+  while (c.st.count * blocks <= off) {
+    off -= c.st.count * blocks;
     c.st = seq_tiles(a, ++c.b, shift);
   }
-  const int64_t off = t0 - base;
-  c.block = static_cast<int>(off / c.st.count);
-  c.tile = static_cast<int>(off % c.st.count);
+  while (off >= c.st.count) {   // (`blocks` is small)
+    off -= c.st.count;
+    ++c.block;
+  }
+  c.tile = off;
   return c;
 }
 // The next entry; true: it belongs to another (sequence, block).
@@ -126,6 +116,16 @@ __device__ __forceinline__ bool advance(const PagedAttnArgs& a, Cursor& c, int s
     while (c.st.count == 0);
   }
   return true;
+}
+
+// What a unit leaves behind: its first (sequence, block) in slot 2u of the partial results if that began or goes on in another
+// unit, its last in slot 2u + 1 if that is another one and goes on in the next.  Whoever holds the beginning of one that goes on
+// says so for the kernel that joins the parts: {parts, sequence, block, slot of the first part}; the others are the slots
+// 2 (u + 1), 2 (u + 2), ...
+__device__ __forceinline__ void say_parts(const PagedAttnArgs& a, int unit, const Cursor& last, bool begins_here, bool first) {
+  const int rest = last.st.count - (last.tile + 1);
+  const bool goes_on = begins_here && rest > 0;
+  a.parts[unit] = make_int4(goes_on ? 1 + (rest + last.per - 1) / last.per : 0, last.b, last.block, 2 * unit + (first ? 0 : 1));
 }
 
 }  // namespace paged

@@ -93,7 +93,10 @@ __global__ void __launch_bounds__(32 * kWarps, 1) paged_attn_kernel(PagedAttnArg
   }
 
   Cursor cur = paged::first_entry(a, blockIdx.x, shift, blocks, lane);
-  if (cur.left == 0) return;
+  if (cur.left == 0) {
+    if (tid == 0) a.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
+    return;
+  }
   const bool first_is_start = cur.tile == 0;   // the unit's first entry begins its (sequence, block)
   Cursor ahead = cur;
   const int page_mask = (1 << a.page_shift) - 1;
@@ -407,6 +410,7 @@ __global__ void __launch_bounds__(32 * kWarps, 1) paged_attn_kernel(PagedAttnArg
     copy(stage == 0 ? S::kStages - 1 : stage - 1);   // the stage of the strip before
     stage = stage == S::kStages - 1 ? 0 : stage + 1;
     const bool last_of_seq = cur.tile + 1 == cur.st.count;
+    if (cur.left == 1 && tid == 0) paged::say_parts(a, blockIdx.x, cur, from_start, first);
     if (last_of_seq || cur.left == 1) {
       finish(from_start, last_of_seq, first);
       first = false;
@@ -423,94 +427,144 @@ __global__ void __launch_bounds__(32 * kWarps, 1) paged_attn_kernel(PagedAttnArg
 }
 
 // ---- parts of a sequence that several units worked on -------------------------------------------------
-// Unit u left its first (sequence, block) in slot 2u if that began or goes on in another unit, its last in slot 2u + 1 if that goes on
-// in the next.  A block joins some dims of one query head: weights 2^(lse_i - max) / sum over the parts, in the parts' order.
-constexpr int kJoinThreads = 256;
+// Weights 2^(lse_i - max) / sum over the parts, added in the parts' order.  A warp joins a row of few parts; the warps of a block share
+// 128 dims of a row of many (one long sequence is 148 parts: 300 KB of a latent row).
+constexpr int kJoinWarps = 8, kFewParts = 8, kManyDims = 128;
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedAttnArgs a, int shift, int blocks, int dims) {
-  __shared__ int64_t sums[2][kJoinThreads / 32];
-  __shared__ float wgt[kMaxPagedUnits];
-  __shared__ float4 acc[kJoinThreads];
+__device__ __forceinline__ void store4(T* out, const float4& x) {
+  uint2 w;
+  if constexpr (__is_same(T, __nv_bfloat16)) w = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
+  else w = make_uint2(pack_f16(x.x, x.y), pack_f16(x.z, x.w));
+  *reinterpret_cast<uint2*>(out) = w;
+}
+template <typename T>
+__global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(PagedAttnArgs a, int rows) {
+  __shared__ int4 parts[kMaxPagedUnits];
+  __shared__ int upto[kMaxPagedUnits];     // rounds of a block for the owners up to this one
+  __shared__ float4 acc[kJoinWarps][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int b = blockIdx.x, h = blockIdx.y, d0 = blockIdx.z * dims;
   pdl_wait();
   pdl_launch_dependents();
-  int64_t all = 0, before = 0;
-  for (int i = tid; i < a.batch; i += kJoinThreads) {
-    const int64_t c = paged::seq_tiles(a, i, shift).count;
-    all += c;
-    if (i < b) before += c;
-  }
-  all = paged::warp_sum(all);
-  before = paged::warp_sum(before);
-  if (lane == 0) {
-    sums[0][warp] = all;
-    sums[1][warp] = before;
-  }
-  __syncthreads();
-  all = before = 0;
-#pragma unroll
-  for (int i = 0; i < kJoinThreads / 32; ++i) {
-    all += sums[0][i];
-    before += sums[1][i];
-  }
-  const int count = paged::seq_tiles(a, b, shift).count;
-  if (count == 0) return;
-  const int rows = a.H / blocks, block = h / rows, row = h - block * rows;   // rows of a unit's partial results
-  const paged::List l = paged::list_of(all * blocks, a);
-  const int64_t s = before * blocks + static_cast<int64_t>(block) * count, e = s + count - 1;
-  const int u0 = static_cast<int>(s / l.per), n = static_cast<int>(e / l.per) - u0 + 1;
-  if (n == 1) return;   // its unit has written the result
-  const int slot0 = 2 * u0 + (s % l.per == 0 ? 0 : 1);
-  auto slot = [&](int i) -> int64_t { return i == 0 ? slot0 : 2 * (u0 + i); };
+  for (int i = tid; i < a.units; i += 32 * kJoinWarps) parts[i] = __ldcg(a.parts + i);
+  // (units that gave up on a wait have left nothing, and nothing said about it)
+  if (__syncthreads_or(a.status != nullptr && *reinterpret_cast<const volatile int*>(a.status) != 0)) return;
+  const int chunks = max(a.dv / kManyDims, 1), chunk_dims = min(a.dv, kManyDims);
+  auto rounds = [&](int n) { return n == 0 ? 0 : n <= kFewParts ? (rows + kJoinWarps - 1) / kJoinWarps : rows * chunks; };
   if (warp == 0) {
-    float m = -INFINITY;
-    for (int i = lane; i < n; i += 32) {
-      wgt[i] = __ldcg(a.part_lse + slot(i) * rows + row);
-      m = fmaxf(m, wgt[i]);
-    }
+    int sum = 0;
+    for (int i0 = 0; i0 < a.units; i0 += 32) {
+      int x = i0 + lane < a.units ? rounds(parts[i0 + lane].x) : 0;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float ref = m > -INFINITY ? m : 0.f;
-    float den = 0.f;
-    for (int i = lane; i < n; i += 32) {
-      wgt[i] = exp2f(wgt[i] - ref);
-      den += wgt[i];
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (i0 + lane < a.units) upto[i0 + lane] = sum + x;
+      sum += __shfl_sync(0xffffffffu, x, 31);
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-    const float inv = den > 0.f || den != den ? 1.f / den : 0.f;
-    for (int i = lane; i < n; i += 32) wgt[i] *= inv;
-    if (lane == 0 && d0 == 0 && a.lse != nullptr)
-      a.lse[static_cast<int64_t>(b) * a.H + h] = den > 0.f || den != den ? (m + log2f(den)) / paged::kLog2e : -INFINITY;
   }
   __syncthreads();
-  // a row of `dims` / 4 threads per part, as many parts at a time as there are threads
-  const int per_row = dims / 4, ways = kJoinThreads / per_row, way = tid / per_row, c = tid % per_row;
-  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float* src = a.part_out + static_cast<int64_t>(row) * a.dv + d0 + 4 * c;
-#pragma unroll 8
-  for (int i = way; i < n; i += ways) {
-    const float4 y = __ldcg(reinterpret_cast<const float4*>(src + slot(i) * rows * a.dv));
-    const float w = wgt[i];
-    x.x += w * y.x; x.y += w * y.y; x.z += w * y.z; x.w += w * y.w;
-  }
-  acc[tid] = x;
-  __syncthreads();
-  if (way == 0) {
-    for (int i = 1; i < ways; ++i) {
-      const float4 y = acc[i * per_row + c];
-      x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+  const int total = upto[a.units - 1];
+  for (int it = blockIdx.x; it < total; it += gridDim.x) {   // block-uniform
+    int lo = 0, hi = a.units - 1;   // the first owner with upto > it
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (upto[mid] > it) hi = mid;
+      else lo = mid + 1;
     }
-    T* out = static_cast<T*>(a.out) + b * a.ld_out + static_cast<int64_t>(h) * a.dv + d0 + 4 * c;
-    uint2 w;
-    if constexpr (__is_same(T, __nv_bfloat16)) w = make_uint2(pack_bf16(x.x, x.y), pack_bf16(x.z, x.w));
-    else w = make_uint2(pack_f16(x.x, x.y), pack_f16(x.z, x.w));
-    *reinterpret_cast<uint2*>(out) = w;
+    const int4 own = parts[lo];
+    const int n = own.x, round = it - (lo > 0 ? upto[lo - 1] : 0);
+    auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (lo + i); };
+    // the weights of the parts of a row, a lane's being those of parts lane, lane + 32, ...
+    constexpr int kMine = (kMaxPagedUnits + 31) / 32;
+    auto weights = [&](int row, float (&w)[kMine], float* lse) {
+      float m = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        w[k] = 32 * k + lane < n ? __ldcg(a.part_lse + slot(32 * k + lane) * rows + row) : -INFINITY;
+        m = fmaxf(m, w[k]);
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const float ref = m > -INFINITY ? m : 0.f;
+      float den = 0.f;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        w[k] = exp2f(w[k] - ref);
+        den += w[k];
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
+      const bool some = den > 0.f || den != den;
+      const float inv = some ? 1.f / den : 0.f;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) w[k] *= inv;
+      *lse = some ? (m + log2f(den)) / paged::kLog2e : -INFINITY;
+    };
+    float w[kMine], lse;
+    if (n <= kFewParts) {
+      const int row = round * kJoinWarps + warp;
+      if (row < rows) {   // whole warps
+        weights(row, w, &lse);
+        const int h = own.z * rows + row;
+        if (lane == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(own.y) * a.H + h] = lse;
+        for (int d = 4 * lane; d < a.dv; d += 128) {
+          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < kFewParts; ++i) {
+            if (i < n) {
+              const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part_out + (slot(i) * rows + row) * a.dv + d));
+              const float wi = __shfl_sync(__activemask(), w[0], i);
+              x.x += wi * y.x; x.y += wi * y.y; x.z += wi * y.z; x.w += wi * y.w;
+            }
+          }
+          store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d, x);
+        }
+      }
+    } else {
+      const int row = round / chunks, d0 = (round - row * chunks) * chunk_dims;
+      const int h = own.z * rows + row;
+      weights(row, w, &lse);
+      if (tid == 0 && d0 == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(own.y) * a.H + h] = lse;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      const bool on = 4 * lane < chunk_dims;
+      const float* src = a.part_out + static_cast<int64_t>(row) * a.dv + d0 + (on ? 4 * lane : 0);
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {   // parts 32 k + 8 j + warp
+          const int i = 32 * k + 8 * j + warp;
+          const float wi = __shfl_sync(0xffffffffu, w[k], 8 * j + warp);
+          if (i < n) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(src + slot(i) * rows * a.dv));
+            x.x += wi * y.x; x.y += wi * y.y; x.z += wi * y.z; x.w += wi * y.w;
+          }
+        }
+      }
+      __syncthreads();   // (the round before has been read)
+      acc[warp][lane] = x;
+      __syncthreads();
+      if (warp == 0) {
+#pragma unroll
+        for (int i = 1; i < kJoinWarps; ++i) {
+          const float4 y = acc[i][lane];
+          x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        }
+        if (on) store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d0 + 4 * lane, x);
+      }
+    }
   }
 }
 
 int heads_shift_of(int G) { return G % 8 == 0 ? 3 : G % 4 == 0 ? 2 : G % 2 == 0 ? 1 : 0; }
+
+static cudaError_t launch_paged_join(const PagedAttnArgs& a, int blocks, cudaStream_t st, int64_t* n_launch) {
+  auto kernel = a.fp16 ? paged_join_kernel<__half> : paged_join_kernel<__nv_bfloat16>;
+  cudaError_t e = launch_pdl(kernel, dim3(4 * a.units), dim3(32 * kJoinWarps), 0, st, a, a.H / blocks);
+  if (e == cudaSuccess) e = cudaGetLastError();
+  if (e == cudaSuccess) ++*n_launch;
+  return e;
+}
 
 template <typename T, int D, bool kE4M3>
 cudaError_t launch_t(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
@@ -524,7 +578,7 @@ cudaError_t launch_t(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch)
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   ++*n_launch;
-  return launch_paged_join(a, S::kRowShift + 3 - hs, a.G >> hs, st, n_launch);
+  return launch_paged_join(a, a.G >> hs, st, n_launch);
 }
 template <typename T>
 cudaError_t launch_d(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
@@ -534,18 +588,12 @@ cudaError_t launch_d(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch)
 
 }  // namespace
 
-int paged_rows(int latent, int H, int G) { return latent ? H : (H / G) << heads_shift_of(G); }
-
-cudaError_t launch_paged_join(const PagedAttnArgs& a, int shift, int blocks, cudaStream_t st, int64_t* n_launch) {
-  // few rows: several blocks for the dims of one
-  int dims = a.dv;
-  while (dims > 64 && static_cast<int64_t>(a.batch) * a.H * (a.dv / dims) < 4 * a.units) dims /= 2;
-  auto kernel = a.fp16 ? paged_join_kernel<__half> : paged_join_kernel<__nv_bfloat16>;
-  cudaError_t e = launch_pdl(kernel, dim3(a.batch, a.H, a.dv / dims), dim3(kJoinThreads), 0, st, a, shift, blocks, dims);
-  if (e == cudaSuccess) e = cudaGetLastError();
-  if (e == cudaSuccess) ++*n_launch;
-  return e;
+int paged_rows(int latent, int H, int G) { return latent ? 64 : (H / G) << heads_shift_of(G); }
+int64_t paged_entries(const PagedAttnArgs& a) {
+  const int hs = heads_shift_of(a.G), keys = a.latent ? 64 : 16 << (3 - hs);   // (at least so many keys a tile)
+  return static_cast<int64_t>(a.batch) * (a.max_len / keys + 2) * (a.G >> hs);
 }
+
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
   return a.fp16 ? launch_d<__half>(a, st, n_launch) : launch_d<__nv_bfloat16>(a, st, n_launch);

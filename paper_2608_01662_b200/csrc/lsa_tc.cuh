@@ -105,6 +105,13 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+      : "memory");
+}
+
 // Four rows of a 2-D tensor (row numbers r0..r3, any order, this GPU's memory), columns c0 .. c0 + box width - 1 of
 // each, land as four consecutive rows at `dst`.  The tensor map's box must be one row high.  c0 * element size must
 // be a multiple of 16 bytes; with a 128-byte swizzle `dst` must be 512-byte aligned for the rows to take their place
@@ -374,5 +381,9 @@ bool make_map_bf16_rows(CUtensorMap* map, const void* base, uint64_t cols, uint6
 // A bf16 matrix [rows, ld] seen as [n_blocks of 64 columns][rows][64 columns]: one box (coordinates 0, row, 0) brings
 // box_rows rows x n_blocks column blocks, each block a 128-byte swizzled tile of its own, block after block.
 bool make_map_bf16_tile(CUtensorMap* map, const void* base, uint64_t ld, uint64_t rows, uint32_t box_rows, uint32_t n_blocks);
+// 16-bit rows of `cols` (a multiple of 64) elements, `rows` of them in each of `groups` groups `ld` elements apart, seen as
+// [group][block of 64 columns][row][64 columns]: one box (coordinates 0, row, 0, group) brings box_rows rows x all column blocks, each block
+// a 128-byte swizzled tile of its own; rows past a group's last are zeros.
+bool make_map_16bit_groups(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t groups, uint64_t ld, uint32_t box_rows);
 
 }  // namespace lsa
