@@ -319,6 +319,28 @@ bool make_map_bf16_tile(CUtensorMap* map, const void* base, uint64_t ld, uint64_
             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+bool make_map_16bit_blocks(CUtensorMap* map, const void* base, uint64_t n_all, uint64_t rows, uint64_t ld, uint32_t box_rows, uint32_t n_box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t dims[3] = {64, rows, n_all};
+  const cuuint64_t strides[2] = {ld * 2, 128};
+  const cuuint32_t box[3] = {64, box_rows, n_box};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+bool make_map_u8_blocks(CUtensorMap* map, const void* base, uint32_t cols, uint64_t n_all, uint64_t rows, uint64_t ld, uint32_t box_rows, uint32_t n_box) {
+  EncodeTiledFn fn = encode_tiled_fn();
+  if (fn == nullptr || (cols != 64 && cols != 128)) return false;
+  const cuuint64_t dims[3] = {cols, rows, n_all};
+  const cuuint64_t strides[2] = {ld, cols};
+  const cuuint32_t box[3] = {cols, box_rows, n_box};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            cols == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 bool make_map_16bit_groups(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t groups, uint64_t ld, uint32_t box_rows) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;

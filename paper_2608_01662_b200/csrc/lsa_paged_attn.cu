@@ -1,16 +1,22 @@
 // lsa_paged_attn for caches with separate keys and values: one query per sequence, up to 16 query heads per KV head.
 //
 // A query head's 64 or 128 dims meet each cached key and value once: at most 16 flop per byte read, so the kernel has to keep
-// HBM busy and the products have to stay out of its way.  The query heads of a KV head are the 16 rows of m16n8k16 MMAs.  A
-// warp works alone: it copies strips of 16 or 32 consecutive tokens of one KV head (4 KB of keys, 4 KB of values) into a ring of
-// its own by cp.async, and keeps the running maximum, sum and output of its strips in registers, so that no warp waits for
-// another until the end of a sequence.  A tile is what the eight warps of a block take in one go: all the KV heads of a block
-// (up to eight; a row of the cache is then read whole) times as many strips as make up eight.
+// HBM busy and everything else has to stay out of its way.  Both products are m16n8k16 MMAs with the cache as the A operand and the
+// heads as the eight columns: S^T = K Q^T (16 tokens x 8 heads) and O^T = V^T P^T (16 dims x 8 heads).  The other way round the
+// heads are 16 rows, of which groups of 4 or 8 heads leave most empty: twice the MMAs and twice the registers of O.
+//
+// A tile is eight strips of 16 or 32 tokens of one KV head each: all KV heads of a block (up to eight; a row of the cache is then read
+// whole) times as many strips as make up eight.  One warp copies tiles by TMA, a box per cache page, keys and values (32 KB
+// each) in turn, into a ring of six slots; eight warps take a strip of every tile each and keep the running maximum, sum and
+// output of their strips in registers, so that they meet only at the end of a sequence.  (With the copies issued by the warps
+// that use them, half of the instructions were the bookkeeping of rings and pages: 400 per strip of 16 tokens where the
+// products take 50.)
 //
 // e4m3 caches: a code is exact in fp16, and so is a query scaled by a power of two of its own head, so the scores' products
 // are fp16 MMAs of codes and the scale of a key is applied to the score.  A value's scale is applied to its weight before that is
 // rounded to bf16 (which has the range for any scale); the codes become bf16, exactly.
 #include "lsa_paged.cuh"
+#include "lsa_tc.cuh"
 
 namespace lsa {
 
@@ -18,32 +24,24 @@ namespace {
 
 using paged::Cursor;
 using paged::exp2_fast;
-using paged::SeqTiles;
 
-constexpr int kWarps = 8;
-constexpr float kRescaleGap = 8.f;   // the output is rescaled only when a row's maximum grows by more than 2^8
+constexpr int kWarps = 8, kThreads = 32 * (kWarps + 1);   // and the one that copies
+constexpr int kRing = 6;
+constexpr float kRescaleGap = 8.f;   // the output is rescaled only when a head's maximum grows by more than 2^8
 
-template <int D, bool kE4M3>
-struct Strip {
-  static constexpr int kElem = kE4M3 ? 1 : 2, kRowBytes = D * kElem;
-  static constexpr int kRows = 4096 / kRowBytes < 32 ? 4096 / kRowBytes : 32;
-  static constexpr int kBytes = kRows * kRowBytes;                 // of keys, and of values
-  static constexpr int kScaleBytes = kE4M3 ? 2 * kRows * 4 : 0;
-  static constexpr int kStage = 2 * kBytes + kScaleBytes;
-  static constexpr int kStages = kBytes == 4096 ? 3 : 5;
-  static constexpr int kRowShift = kRows == 32 ? 5 : 4;
-  static constexpr int kRing = kWarps * kStages * kStage;
-  static constexpr int kMergePitch = 36;                           // floats: 32 dims of a row and a gap
-  static constexpr int kMerge = kWarps * 16 * kMergePitch * 4;
-  static constexpr int kSmem = kRing + kMerge + kWarps * 16 * 8;
+// kTiles: groups of eight query heads per KV head (1 or 2).
+template <int D, bool kE4M3, int kTiles>
+struct Shape {
+  static constexpr int kRowBytes = D * (kE4M3 ? 1 : 2);            // of a head
+  static constexpr int kBlockBytes = kRowBytes < 128 ? 64 : 128;   // columns of a TMA box lie in blocks of this many bytes
+  static constexpr int kBlocks = kRowBytes / kBlockBytes;          // of a head
+  static constexpr int kRows = kRowBytes == 256 ? 16 : 32, kRowShift = kRows == 32 ? 5 : 4;   // of a strip
+  static constexpr int kBytes = kWarps * kRows * kRowBytes;        // of a tile's keys, and of its values: one slot each
+  static constexpr int kScales = kE4M3 ? kWarps * kRows * 4 : 0;
+  static constexpr int kMergePitch = 34;                           // floats: 32 dims of a head and a gap
+  static constexpr int kMerge = kWarps * 8 * kTiles * kMergePitch * 4;
+  static constexpr int kSmem = 1024 + kRing * (kBytes + kScales) + kMerge + kWarps * 8 * kTiles * 8 + 2 * kRing * 8;
 };
-
-// 16-byte unit u of row r of a strip: the units that one ldmatrix phase reads (eight rows) lie in different banks.
-template <int kRowBytes>
-__device__ __forceinline__ uint32_t unit_at(int r, int u) {
-  if constexpr (kRowBytes == 64) return (r >> 1) * 128 + (((((r & 1) << 2) | u) ^ ((r >> 1) & 7)) << 4);
-  else return swz<kRowBytes>(r, u);
-}
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile(
@@ -51,379 +49,506 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+template <bool kF16>
+__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (kF16) mma_f16(d, a, b0, b1);
+  else mma_bf16(d, a, b0, b1);
+}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint32_t two) {
-  __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3);
-  return static_cast<uint32_t>(h.x) | (static_cast<uint32_t>(h.y) << 16);
+// Transposes an 8x8 matrix of 16-bit elements held as an MMA fragment.
+__device__ __forceinline__ uint32_t transposed(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, int src_bytes) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes));
+__device__ __forceinline__ uint32_t e4m3x2_to_f16x2(uint16_t two) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(two));
+  return r;
 }
+template <int kBytes>
+__device__ __forceinline__ void cp_async_ca(uint32_t dst, const void* src, int src_bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(dst), "l"(src), "n"(kBytes), "r"(src_bytes));
+}
+// The barrier counts this thread once its earlier cp.async have landed (its count includes the arrival).
+__device__ __forceinline__ void cp_async_arrive(uint32_t bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void workers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(32 * kWarps) : "memory"); }
 
-// heads: KV heads that a block works on at the same time (8, 4, 2 or 1, a divisor of G); strips: strips of a tile (8 / heads).
-template <typename T, int D, bool kE4M3>
-__global__ void __launch_bounds__(32 * kWarps, 1) paged_attn_kernel(PagedAttnArgs a, int heads_shift) {
-  using S = Strip<D, kE4M3>;
-  constexpr bool kF16 = sizeof(T) == 2 && !__is_same(T, __nv_bfloat16);
-  constexpr int R = S::kRows, kTiles = R / 8;       // n-tiles of a strip's scores
-  extern __shared__ __align__(128) uint8_t smem[];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int g4 = lane >> 2, t4 = lane & 3;
+// heads_shift: log2 of the KV heads that a block works on at the same time (8, 4, 2 or 1, a divisor of G).
+template <typename T, int D, bool kE4M3, int kTiles>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, PagedAttnArgs a, int heads_shift) {
+  using S = Shape<D, kE4M3, kTiles>;
+  constexpr bool kF16 = !__is_same(T, __nv_bfloat16);
+  constexpr bool kQkF16 = kF16 || kE4M3, kPvF16 = kF16 && !kE4M3;
+  constexpr int R = S::kRows, kSub = R / 16, kHeadsOf = 8 * kTiles;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  float* const scales = reinterpret_cast<float*>(ring + kRing * S::kBytes);     // [slot][row of the tile][head]
+  float* const merge = scales + kRing * S::kScales / 4;
+  float2* const ml = reinterpret_cast<float2*>(merge + S::kMerge / 4);          // {maximum, sum} per warp and head
+  const uint32_t full = smem_u32(ml + kWarps * kHeadsOf), empty = full + 8 * kRing;
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int strip_shift = 3 - heads_shift, n_strips = 1 << strip_shift;
-  const int head_l = warp >> strip_shift, strip = warp & (n_strips - 1);
   const int shift = S::kRowShift + strip_shift;     // keys of a tile
   const int blocks = a.G >> heads_shift;
-  const int group = a.H / a.G;
-  uint8_t* const ring = smem + warp * S::kStages * S::kStage;
-  float* const merge = reinterpret_cast<float*>(smem + S::kRing);
-  float2* const ml = reinterpret_cast<float2*>(smem + S::kRing + S::kMerge);   // {maximum, sum} per warp and row
+  const int box_shift = min(shift, a.page_shift);   // keys of a box
 
+  if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&v_map) : "memory");
+    for (int i = 0; i < kRing; ++i) {
+      tc::mbar_init(full + 8 * i, kE4M3 ? 33 : 1);
+      tc::mbar_init(empty + 8 * i, kWarps);
+    }
+    tc::fence_mbar_init();
+  }
   pdl_wait();
   pdl_launch_dependents();
-
-  // sequences without tokens belong to no tile
-  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-    if (paged::seq_length(a, b, tid == 0) > 0) continue;
-    T* out = static_cast<T*>(a.out) + b * a.ld_out;
-    for (int i = tid; i < a.H * D; i += 32 * kWarps) out[i] = T(0.f);
-    for (int i = tid; i < a.H && a.lse != nullptr; i += 32 * kWarps) a.lse[static_cast<int64_t>(b) * a.H + i] = -INFINITY;
-  }
-
+  const bool raised = tc::status_raised(a.status);
   Cursor cur = paged::first_entry(a, blockIdx.x, shift, blocks, lane);
-  if (cur.left == 0) {
-    if (tid == 0) a.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
-    return;
-  }
-  const bool first_is_start = cur.tile == 0;   // the unit's first entry begins its (sequence, block)
-  Cursor ahead = cur;
-  const int page_mask = (1 << a.page_shift) - 1;
+  const bool dead = __syncthreads_or(raised) != 0;   // the same in all threads
+  if (dead) return;
 
-  // ---- copies: the strip at `ahead`, whose page numbers were fetched one call before
-  int pages[R / 16];
-  auto fetch_pages = [&]() {
-    const int s0 = ahead.st.first_key(ahead.tile, shift) + strip * R;
-#pragma unroll
-    for (int h = 0; h < R / 16; ++h) {
-      pages[h] = -1;
-      if (ahead.left > 0 && ahead.st.any_seen(s0 + 16 * h, 16)) {
-        const int p = a.page_table[ahead.b * a.pt_stride + ((s0 + 16 * h) >> a.page_shift)];
-        if (p >= 0 && p < a.n_pages) pages[h] = p;
-        else paged::report_index(a.notice);
+  if (warp == kWarps) {
+    // ================= copies =================
+    const int page_mask = (1 << a.page_shift) - 1;
+    const int beyond = static_cast<int>(static_cast<int64_t>(max(a.n_pages, 1)) << a.page_shift);   // the first row past the pool: rows of zeros
+    const int box_bytes = (S::kBytes >> shift) << box_shift;   // (a tile's bytes over its keys, times a box's)
+    const int n_boxes = 1 << (shift - box_shift);
+    // a lane's box of the tile at the cursor: its cache row; past the pool if its page is not one, -1 if nobody sees its keys
+    auto row_of = [&]() -> int {
+      if (cur.left <= 0 || lane >= n_boxes) return -1;
+      const int s0 = cur.st.first_key(cur.tile, shift) + (lane << box_shift);
+      if (!cur.st.any_seen(s0, 1 << box_shift)) return -1;
+      const int p = a.page_table[cur.b * a.pt_stride + (s0 >> a.page_shift)];
+      if (p < 0 || p >= a.n_pages) {
+        paged::report_index(a.notice);
+        return beyond;
       }
-    }
-  };
-  auto copy = [&](int stage) {
-    if (ahead.left > 0) {
-      const int s0 = ahead.st.first_key(ahead.tile, shift) + strip * R;
-      const int g = (ahead.block << heads_shift) + head_l;
-      const uint32_t dst = smem_u32(ring + stage * S::kStage);
-      const uint8_t* kp = static_cast<const uint8_t*>(a.k_pool);
-      const uint8_t* vp = static_cast<const uint8_t*>(a.v_pool);
-      constexpr int kUnits = S::kRowBytes / 16, kAtOnce = 32 / kUnits;   // units of a row; rows that the warp copies with one instruction
-      const int u = lane % kUnits, r0 = lane / kUnits;
+      return (p << a.page_shift) + (s0 & page_mask);
+    };
+    int row = row_of(), slot = 0;
+    uint32_t use = 0;
+    const int entries = cur.left;
+    int issued = 0;
+    bool alive = true;
+    for (int g = 0; g < entries && alive; ++g) {
+      const int this_row = row, head0 = cur.block << heads_shift;
+      paged::advance(a, cur, shift, blocks);
+      row = row_of();   // (its page number is on its way while this tile waits for its slots)
+      const int n_here = __popc(__ballot_sync(0xffffffffu, this_row >= 0));
 #pragma unroll
-      for (int h = 0; h < R / 16; ++h) {
-        const int64_t row0 = (static_cast<int64_t>(max(pages[h], 0)) << a.page_shift) + ((s0 + 16 * h) & page_mask);
-        const uint8_t* ks = kp + (row0 + r0) * a.ld_k * S::kElem + g * S::kRowBytes + u * 16;
-        const uint8_t* vs = vp + (row0 + r0) * a.ld_v * S::kElem + g * S::kRowBytes + u * 16;
-#pragma unroll
-        for (int i = 0; i < 16 / kAtOnce; ++i) {
-          const int r = 16 * h + i * kAtOnce + r0;
-          const int bytes = pages[h] >= 0 && ahead.st.seen(s0 + r) ? 16 : 0;   // what is not seen is a row of zeros
-          cp_async16(dst + unit_at<S::kRowBytes>(r, u), ks + static_cast<int64_t>(i * kAtOnce) * a.ld_k * S::kElem, bytes);
-          cp_async16(dst + S::kBytes + unit_at<S::kRowBytes>(r, u), vs + static_cast<int64_t>(i * kAtOnce) * a.ld_v * S::kElem, bytes);
+      for (int kv = 0; kv < 2; ++kv) {
+        alive = alive && __all_sync(0xffffffffu, tc::mbar_wait(empty + 8 * slot, use ^ 1u, a.status));
+        if (!alive) break;
+        const uint32_t bar = full + 8 * slot;
+        if (lane == 0) tc::mbar_expect_tx(bar, static_cast<uint32_t>(n_here * box_bytes));
+        __syncwarp();
+        if (this_row >= 0)
+          tc::tma_load_3d(smem_u32(ring) + slot * S::kBytes + lane * box_bytes, kv == 0 ? &k_map : &v_map, 0, this_row, head0 * S::kBlocks, bar);
+        if constexpr (kE4M3) {
+          const float* src = kv == 0 ? a.k_scale : a.v_scale;
+          const uint32_t dst = smem_u32(scales) + slot * S::kScales;
+          for (int j = 0; j < n_boxes; ++j) {   // rows of 4, 8, 16 or 32 bytes, a lane each
+            const int r0 = __shfl_sync(0xffffffffu, this_row, j);
+            if (r0 < 0) continue;
+            for (int i = lane; i < 1 << box_shift; i += 32) {
+              const int r = (j << box_shift) + i;
+              const float* s = src + (r0 < beyond ? static_cast<int64_t>(r0 + i) * a.G + head0 : 0);
+              const bool there = r0 < beyond;
+              if (heads_shift == 0) cp_async_ca<4>(dst + r * 4, s, there ? 4 : 0);
+              else if (heads_shift == 1) cp_async_ca<8>(dst + r * 8, s, there ? 8 : 0);
+              else
+                for (int h = 0; h < 1 << (heads_shift - 2); ++h) cp_async_ca<16>(dst + (r << (heads_shift + 2)) + 16 * h, s + 4 * h, there ? 16 : 0);
+            }
+          }
+          cp_async_arrive(bar);
+        }
+        __syncwarp();
+        ++issued;
+        if (++slot == kRing) {
+          slot = 0;
+          use ^= 1u;
         }
       }
-      if constexpr (kE4M3) {
-        static_assert(R == 32, "a lane per row of scales");
-        const int p = lane < 16 ? pages[0] : pages[R / 16 - 1];
-        const int64_t row = (static_cast<int64_t>(max(p, 0)) << a.page_shift) + ((s0 + lane) & page_mask);
-        const int bytes = p >= 0 && ahead.st.seen(s0 + lane) ? 4 : 0;
-        cp_async4(dst + 2 * S::kBytes + lane * 4, a.k_scale + row * a.G + g, bytes);
-        cp_async4(dst + 2 * S::kBytes + R * 4 + lane * 4, a.v_scale + row * a.G + g, bytes);
-      }
-      paged::advance(a, ahead, shift, blocks);
-      fetch_pages();
     }
-    cp_async_commit();
-  };
+    // every copy has landed before the block ends, also if somebody gave up on a wait
+    for (int i = max(issued - kRing, 0); i < issued; ++i) (void)tc::mbar_wait(full + 8 * (i % kRing), static_cast<uint32_t>(i / kRing) & 1u, nullptr);
+    return;
+  }
 
-  // ---- the state of a (sequence, block): query fragments, output, maxima, sums
-  uint32_t qf[D / 16][4];
-  float zs[2];
-  float o[D / 8][4];
-  float m_used[2], l_run[2];
+  // ================= strips =================
+  const int g4 = lane >> 2, t4 = lane & 3;
+  const int head_l = warp >> strip_shift, strip = warp & (n_strips - 1);
+  const int group = a.H / a.G;
+  if (cur.left == 0 && tid == 0) a.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
+
+  // Where the strip lies in a slot: boxes of [block of columns][key][block bytes], 16-byte units XORed as TMA does it, which also keeps the
+  // eight rows that an ldmatrix phase reads in different banks.  A strip of 32 tokens in pages of 16 lies in two boxes.
+  const int block_stride = S::kBlockBytes << box_shift;
+  auto strip_at = [&](int key) -> uint32_t {   // offset of a key of the strip, first block of the head
+    const int k = strip * R + key, j = k >> box_shift, in = k & ((1 << box_shift) - 1);
+    return j * (block_stride * S::kBlocks << heads_shift) + head_l * S::kBlocks * block_stride + in * S::kBlockBytes;
+  };
+  // XOR of the unit index of row r; (rows of a strip are aligned to 16)
+  auto twist = [](int r) -> uint32_t { return S::kBlockBytes == 64 ? ((r >> 1) & 3) << 4 : (r & 7) << 4; };
+  // Addresses of a lane in a slot (without the slot's base), unit 0 or 1: units 2 i and 2 i + 1 further on are an XOR of 32 i.
+  uint32_t k_off[kSub], v_off[kSub];
+  if constexpr (!kE4M3) {
+#pragma unroll
+    for (int j = 0; j < kSub; ++j) {
+      const int rk = 16 * j + (lane & 15), rv = 16 * j + (lane & 7) + ((lane >> 4) << 3);
+      k_off[j] = strip_at(rk) + (static_cast<uint32_t>(lane >> 4) << 4 ^ twist(rk));
+      v_off[j] = strip_at(rv) + (static_cast<uint32_t>((lane >> 3) & 1) << 4 ^ twist(rv));
+    }
+  } else {   // one row of codes per lane, keys and values alike
+    k_off[0] = v_off[0] = strip_at(lane) + twist(lane);
+  }
+
+  // ---- the state of a (sequence, block): query fragments, output, maxima and sums of the heads 8 n + 2 t4, + 1
+  uint32_t qf[kTiles][D / 16][2];
+  float o[kTiles][D / 16][4];
+  float zs[kTiles][2], m_used[kTiles][2], l_run[kTiles][2];
   auto begin = [&]() {
     const int head0 = ((cur.block << heads_shift) + head_l) * group;
     const T* q = static_cast<const T*>(a.q) + cur.b * a.ld_q + static_cast<int64_t>(head0) * D;
-    zs[0] = zs[1] = a.scale2;
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      const bool on = g4 + 8 * r < group;
-      const uint32_t* row = reinterpret_cast<const uint32_t*>(q + (g4 + 8 * r) * D);   // pairs of dims
-      if constexpr (!kE4M3) {
+    for (int n = 0; n < kTiles; ++n) {
+      const bool on = 8 * n + g4 < group;
+      const uint32_t* row = reinterpret_cast<const uint32_t*>(q + (on ? 8 * n + g4 : 0) * D);   // pairs of dims
+      zs[n][0] = zs[n][1] = a.scale2;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          qf[k][r] = on ? row[8 * k + t4] : 0u;
-          qf[k][2 + r] = on ? row[8 * k + 4 + t4] : 0u;
-        }
-      } else {   // dims 16 k + 4 t .. + 3 take the places of the columns 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of step k
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
+      for (int k = 0; k < D / 16; ++k) {
+        if constexpr (!kE4M3) {
+          qf[n][k][0] = on ? row[8 * k + t4] : 0u;
+          qf[n][k][1] = on ? row[8 * k + 4 + t4] : 0u;
+        } else {   // dims 16 k + 4 t .. + 3 take the places of the rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9 of step k
           const uint2 w = on ? *reinterpret_cast<const uint2*>(row + 8 * k + 2 * t4) : make_uint2(0u, 0u);
-          qf[k][r] = w.x;
-          qf[k][2 + r] = w.y;
-        }
-        if constexpr (!kF16) {
-          float top = 0.f;
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[k][2 * h + r]));
-              top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-            }
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          // largest element in [2^14, 2^15): what lies 2^-29 below it still has all its bits
-          const int sh = e5m2_head_shift(top);
-          const float up = __uint_as_float(static_cast<uint32_t>(127 + sh) << 23);
-          zs[r] *= __uint_as_float(static_cast<uint32_t>(127 - sh) << 23);
-#pragma unroll
-          for (int k = 0; k < D / 16; ++k)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[k][2 * h + r]));
-              qf[k][2 * h + r] = pack_f16(f.x * up, f.y * up);
-            }
+          qf[n][k][0] = w.x;
+          qf[n][k][1] = w.y;
         }
       }
-      m_used[r] = -INFINITY;
-      l_run[r] = 0.f;
-    }
+      if constexpr (kE4M3 && !kF16) {
+        float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[n][k][h]));
+            top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // largest element in [2^14, 2^15): what lies 2^-29 below it still has all its bits
+        const int sh = e5m2_head_shift(top);
+        const float up = __uint_as_float(static_cast<uint32_t>(127 + sh) << 23), down = __uint_as_float(static_cast<uint32_t>(127 - sh) << 23);
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[n][k][h]));
+            qf[n][k][h] = pack_f16(f.x * up, f.y * up);
+          }
+        zs[n][0] *= __shfl_sync(0xffffffffu, down, 8 * t4);
+        zs[n][1] *= __shfl_sync(0xffffffffu, down, 8 * t4 + 4);
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        m_used[n][c] = -INFINITY;
+        l_run[n][c] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
+    }
+  };
+
+  int slot = 0;
+  uint32_t use = 0;
+  bool ok = true;
+  auto arrived = [&]() {   // the next slot's bytes are there
+    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(full + 8 * slot, use, a.status));
+  };
+  auto release = [&]() {
+    __syncwarp();
+    if (lane == 0) tc::mbar_arrive(empty + 8 * slot);
+    if (++slot == kRing) {
+      slot = 0;
+      use ^= 1u;
+    }
   };
 
   // ---- one strip
-  auto work = [&](int stage) {
+  auto work = [&]() {
     const int s0 = cur.st.first_key(cur.tile, shift) + strip * R;
-    if (!cur.st.any_seen(s0, R)) return;
-    const uint32_t ks = smem_u32(ring + stage * S::kStage), vs = ks + S::kBytes;
-    float s[kTiles][4];
-#pragma unroll
-    for (int j = 0; j < kTiles; ++j) s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-#pragma unroll
-    for (int k = 0; k < D / 16; ++k) {
-      if constexpr (!kE4M3) {
-#pragma unroll
-        for (int j = 0; j < R / 16; ++j) {
-          uint32_t w[4];
-          ldmatrix_x4(w, ks + unit_at<S::kRowBytes>(16 * j + (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-          if constexpr (kF16) {
-            mma_f16(s[2 * j], qf[k], w[0], w[1]);
-            mma_f16(s[2 * j + 1], qf[k], w[2], w[3]);
-          } else {
-            mma_bf16(s[2 * j], qf[k], w[0], w[1]);
-            mma_bf16(s[2 * j + 1], qf[k], w[2], w[3]);
-          }
-        }
-      } else {
-        uint32_t w[4];   // four codes of a key: dims 16 k + 4 t .. + 3, keys 8 j + lane / 4
-        ldmatrix_x4(w, ks + unit_at<S::kRowBytes>(lane, k));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mma_f16(s[j], qf[k], e4m3x2_to_f16x2(w[j] & 0xffffu), e4m3x2_to_f16x2(w[j] >> 16));
-      }
+    const bool any = cur.st.any_seen(s0, R), partial = !cur.st.all_seen(s0, R);
+    arrived();
+    if (!any) {   // (the slots are waited for and given free all the same: a warp ahead of the others would be counted twice)
+      release();
+      arrived();
+      release();
+      return;
     }
-    // scores in log2 units; the thread's keys are 8 j + 2 t, + 1, its rows g4 and g4 + 8
-    float2 vsc[kTiles];
-    const float* sc = reinterpret_cast<const float*>(ring + stage * S::kStage + 2 * S::kBytes);
+    float s[kSub][kTiles][4];
 #pragma unroll
-    for (int j = 0; j < kTiles; ++j) {
-      float2 ksc = make_float2(1.f, 1.f);
-      if constexpr (kE4M3) {
-        ksc = *reinterpret_cast<const float2*>(sc + 8 * j + 2 * t4);
-        vsc[j] = *reinterpret_cast<const float2*>(sc + R + 8 * j + 2 * t4);
-        s[j][0] *= ksc.x; s[j][1] *= ksc.y; s[j][2] *= ksc.x; s[j][3] *= ksc.y;
-      }
-      s[j][0] *= zs[0]; s[j][1] *= zs[0]; s[j][2] *= zs[1]; s[j][3] *= zs[1];
-    }
-    if (!cur.st.all_seen(s0, R)) {
+    for (int j = 0; j < kSub; ++j)
 #pragma unroll
-      for (int j = 0; j < kTiles; ++j)
+      for (int n = 0; n < kTiles; ++n) s[j][n][0] = s[j][n][1] = s[j][n][2] = s[j][n][3] = 0.f;
+    {
+      const uint32_t kb = smem_u32(ring) + slot * S::kBytes;
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-          if (!cur.st.seen(s0 + 8 * j + 2 * t4 + c)) s[j][c] = s[j][2 + c] = -INFINITY;
-    }
-    float mx[2];
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      float x = fmaxf(s[0][2 * r], s[0][2 * r + 1]);
-#pragma unroll
-      for (int j = 1; j < kTiles; ++j) x = fmaxf(x, fmaxf(s[j][2 * r], s[j][2 * r + 1]));
-      x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-      mx[r] = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-    }
-    const bool grow0 = mx[0] > m_used[0] + kRescaleGap, grow1 = mx[1] > m_used[1] + kRescaleGap;
-    if (__any_sync(0xffffffffu, grow0 || grow1)) {
-      float al[2];
-#pragma unroll
-      for (int r = 0; r < 2; ++r) {
-        al[r] = 1.f;
-        if (r == 0 ? grow0 : grow1) {
-          al[r] = exp2_fast(m_used[r] - mx[r]);   // (the first time: 0)
-          m_used[r] = mx[r];
-        }
-        l_run[r] *= al[r];
-      }
-#pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        o[i][0] *= al[0]; o[i][1] *= al[0]; o[i][2] *= al[1]; o[i][3] *= al[1];
-      }
-    }
-    // (a row whose scores are all -inf so far has no maximum: its weights are 0)
-    const float ref[2] = {m_used[0] > -INFINITY ? m_used[0] : 0.f, m_used[1] > -INFINITY ? m_used[1] : 0.f};
-#pragma unroll
-    for (int j = 0; j < kTiles; ++j) {
-#pragma unroll
-      for (int c = 0; c < 4; ++c) s[j][c] = exp2_fast(s[j][c] - ref[c >> 1]);
-      l_run[0] += s[j][0] + s[j][1];
-      l_run[1] += s[j][2] + s[j][3];
-      if constexpr (kE4M3) {
-        s[j][0] *= vsc[j].x; s[j][1] *= vsc[j].y; s[j][2] *= vsc[j].x; s[j][3] *= vsc[j].y;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < R / 16; ++j) {
-      uint32_t p[4];   // weights of keys 16 j .. + 15: rounded to 16 bits, at most 2^8, their sum kept in fp32 above
-      if constexpr (kF16 && !kE4M3) {
-        p[0] = pack_f16(s[2 * j][0], s[2 * j][1]); p[1] = pack_f16(s[2 * j][2], s[2 * j][3]);
-        p[2] = pack_f16(s[2 * j + 1][0], s[2 * j + 1][1]); p[3] = pack_f16(s[2 * j + 1][2], s[2 * j + 1][3]);
-      } else {
-        p[0] = pack_bf16(s[2 * j][0], s[2 * j][1]); p[1] = pack_bf16(s[2 * j][2], s[2 * j][3]);
-        p[2] = pack_bf16(s[2 * j + 1][0], s[2 * j + 1][1]); p[3] = pack_bf16(s[2 * j + 1][2], s[2 * j + 1][3]);
-      }
-      const int r = 16 * j + (lane & 7) + ((lane >> 3) & 1) * 8;
-#pragma unroll
-      for (int d = 0; d < S::kRowBytes / 32; ++d) {   // two 16-byte units of the rows
-        uint32_t w[4];
-        ldmatrix_x4_trans(w, vs + unit_at<S::kRowBytes>(r, 2 * d + (lane >> 4)));
+      for (int k = 0; k < D / 16; ++k) {
         if constexpr (!kE4M3) {
-          if constexpr (kF16) {
-            mma_f16(o[2 * d], p, w[0], w[1]);
-            mma_f16(o[2 * d + 1], p, w[2], w[3]);
-          } else {
-            mma_bf16(o[2 * d], p, w[0], w[1]);
-            mma_bf16(o[2 * d + 1], p, w[2], w[3]);
+#pragma unroll
+          for (int j = 0; j < kSub; ++j) {
+            uint32_t w[4];
+            ldmatrix_x4(w, (kb + k_off[j] + (k >> 2) * block_stride) ^ ((k & 3) * 32));
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma<kQkF16>(s[j][n], w, qf[n][k][0], qf[n][k][1]);
           }
         } else {
-          // a word: dims 2 n, 2 n + 1 (n = lane / 4) of keys 2 t and 2 t + 1; the even dims are one n-tile, the odd ones another
+          uint32_t c[4];   // four codes of a key: dims 16 k + 4 t .. + 3 of keys 8 i + lane / 4
+          ldmatrix_x4(c, (kb + k_off[0]) ^ (k * 16));
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t lo = w[2 * h], hi = w[2 * h + 1];
-            mma_bf16(o[4 * d + 2 * h], p, e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(lo, 0, 0x4420))),
-                     e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(hi, 0, 0x4420))));
-            mma_bf16(o[4 * d + 2 * h + 1], p, e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(lo, 0, 0x4431))),
-                     e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(hi, 0, 0x4431))));
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t w[4] = {e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j])), e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j + 1])),
+                                   e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j] >> 16)), e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j + 1] >> 16))};
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) mma<kQkF16>(s[j][n], w, qf[n][k][0], qf[n][k][1]);
           }
         }
       }
     }
+    if constexpr (kE4M3) {
+      const float* sc = scales + slot * (S::kScales / 4) + ((strip * R + g4) << heads_shift) + head_l;
+#pragma unroll
+      for (int j = 0; j < kSub; ++j)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const float x = sc[(16 * j + 8 * r) << heads_shift];
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) {
+            s[j][n][2 * r] *= x;
+            s[j][n][2 * r + 1] *= x;
+          }
+        }
+    }
+    release();
+    // the thread's keys are 16 j + g4 and 8 more, its heads 8 n + 2 t4 and the next
+    if (partial) {
+#pragma unroll
+      for (int j = 0; j < kSub; ++j)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          if (!cur.st.seen(s0 + 16 * j + 8 * r + g4)) {
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) s[j][n][2 * r] = s[j][n][2 * r + 1] = -INFINITY;
+          }
+    }
+    // P with the maxima as they are; only where a head has grown too far is its maximum moved before
+    float mx[kTiles][2];
+    bool need = false;
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        float x = fmaxf(s[0][n][c], s[0][n][2 + c]);
+#pragma unroll
+        for (int j = 1; j < kSub; ++j) x = fmaxf(x, fmaxf(s[j][n][c], s[j][n][2 + c]));
+        mx[n][c] = x * zs[n][c];
+        need = need || mx[n][c] > m_used[n][c] + kRescaleGap;
+      }
+    if (__any_sync(0xffffffffu, need)) {
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          float x = mx[n][c];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+          if (x > m_used[n][c] + kRescaleGap) {
+            const float al = exp2_fast(m_used[n][c] - x);   // (the first time: 0)
+            m_used[n][c] = x;
+            l_run[n][c] *= al;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              o[n][i][c] *= al;
+              o[n][i][2 + c] *= al;
+            }
+          }
+        }
+    }
+    float e[kSub][kTiles][4];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      // (a head whose scores are all -inf so far has no maximum: its weights are 0)
+      const float ref[2] = {m_used[n][0] > -INFINITY ? m_used[n][0] : 0.f, m_used[n][1] > -INFINITY ? m_used[n][1] : 0.f};
+#pragma unroll
+      for (int j = 0; j < kSub; ++j)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          e[j][n][x] = exp2_fast(fmaf(s[j][n][x], zs[n][x & 1], -ref[x & 1]));
+          l_run[n][x & 1] += e[j][n][x];
+        }
+    }
+    arrived();
+    uint8_t* const vp = ring + slot * S::kBytes;
+    if constexpr (kE4M3) {
+      const float* sc = scales + slot * (S::kScales / 4) + ((strip * R + g4) << heads_shift) + head_l;
+#pragma unroll
+      for (int j = 0; j < kSub; ++j)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          float x = sc[(16 * j + 8 * r) << heads_shift];
+          if (partial && !cur.st.seen(s0 + 16 * j + 8 * r + g4)) x = 0.f;   // (there may be anything)
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) {
+            e[j][n][2 * r] *= x;
+            e[j][n][2 * r + 1] *= x;
+          }
+        }
+    }
+    uint32_t p[kSub][kTiles][2];   // weights, 16 bits: at most 2^8, their sum kept in fp32
+#pragma unroll
+    for (int j = 0; j < kSub; ++j)
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+          p[j][n][r] = transposed(kPvF16 ? pack_f16(e[j][n][2 * r], e[j][n][2 * r + 1]) : pack_bf16(e[j][n][2 * r], e[j][n][2 * r + 1]));
+    if (partial) {   // rows that nobody sees may hold anything, and 0 x NaN is NaN
+      constexpr int kUnits = S::kRowBytes / 16, kUnitsOf = S::kBlockBytes / 16;
+      for (int i = lane; i < R * kUnits; i += 32) {
+        const int r = i / kUnits, u = i % kUnits;   // (all units of a row: their order does not matter)
+        if (!cur.st.seen(s0 + r)) *reinterpret_cast<uint4*>(vp + strip_at(r) + (u / kUnitsOf) * block_stride + (u % kUnitsOf) * 16) = make_uint4(0u, 0u, 0u, 0u);
+      }
+      tc::fence_proxy_async();   // (the next copy into the slot comes through the async proxy)
+      __syncwarp();
+    }
+    const uint32_t vb = smem_u32(vp);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) {
+      if constexpr (!kE4M3) {
+#pragma unroll
+        for (int j = 0; j < kSub; ++j) {
+          uint32_t w[4];
+          ldmatrix_x4_trans(w, (vb + v_off[j] + (i >> 2) * block_stride) ^ ((i & 3) * 32));
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, p[j][n][0], p[j][n][1]);
+        }
+      } else {
+        // a word: dims 2 g4, 2 g4 + 1 of keys 2 t and 2 t + 1; the even dims are the tile's rows 0-7, the odd ones rows 8-15
+        uint32_t c[4];
+        ldmatrix_x4_trans(c, (vb + v_off[0]) ^ (i * 16));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t w[4] = {e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j], 0, 0x4420))),
+                                 e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j], 0, 0x4431))),
+                                 e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4420))),
+                                 e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4431)))};
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, p[j][n][0], p[j][n][1]);
+        }
+      }
+    }
+    release();
   };
 
   // ---- end of a (sequence, block) for this unit: the strips' parts are put together, 32 dims at a time
   const int64_t slot0 = 2 * static_cast<int64_t>(blockIdx.x);
+  const int n_rows = group << heads_shift;
   auto finish = [&](bool from_start, bool to_end, bool first) {
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 1);
-      l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 2);
-      if (t4 == 0) ml[warp * 16 + g4 + 8 * r] = make_float2(m_used[r], l_run[r]);
-    }
-    __syncthreads();
-    float f[2];
+    for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-    for (int r = 0; r < 2; ++r) {
-      float m = -INFINITY, l = 0.f;
-      const float2* all = ml + (head_l << strip_shift) * 16 + g4 + 8 * r;
-      for (int w = 0; w < n_strips; ++w) m = fmaxf(m, all[16 * w].x);
-      const float ref = m > -INFINITY ? m : 0.f;
-      for (int w = 0; w < n_strips; ++w) l += all[16 * w].y * exp2_fast(all[16 * w].x - ref);
-      f[r] = l > 0.f || l != l ? exp2_fast(m_used[r] - ref) / l : 0.f;
-      const int row = g4 + 8 * r, h = ((cur.block << heads_shift) + head_l) * group + row;
-      if (strip == 0 && t4 == 0 && row < group) {
-        const float lse2 = l > 0.f || l != l ? m + log2f(l) : -INFINITY;
-        if (from_start && to_end) {
-          if (a.lse != nullptr) a.lse[static_cast<int64_t>(cur.b) * a.H + h] = lse2 / paged::kLog2e;
-        } else {
-          a.part_lse[(slot0 + (first ? 0 : 1)) * (group << heads_shift) + head_l * group + row] = lse2;
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l_run[n][c] += __shfl_xor_sync(0xffffffffu, l_run[n][c], d);
+        if (g4 == 0) ml[warp * kHeadsOf + 8 * n + 2 * t4 + c] = make_float2(m_used[n][c], l_run[n][c]);
+      }
+    workers_sync();
+    float f[kTiles][2];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const int row = 8 * n + 2 * t4 + c;
+        float m = -INFINITY, l = 0.f;
+        const float2* all = ml + (head_l << strip_shift) * kHeadsOf + row;
+        for (int w = 0; w < n_strips; ++w) m = fmaxf(m, all[kHeadsOf * w].x);
+        const float ref = m > -INFINITY ? m : 0.f;
+        for (int w = 0; w < n_strips; ++w) l += all[kHeadsOf * w].y * exp2_fast(all[kHeadsOf * w].x - ref);
+        const bool some = l > 0.f || l != l;
+        f[n][c] = some ? exp2_fast(m_used[n][c] - ref) / l : 0.f;
+        if (strip == 0 && g4 == 0 && row < group) {
+          const float lse2 = some ? m + log2f(l) : -INFINITY;
+          if (from_start && to_end) {
+            if (a.lse != nullptr) a.lse[static_cast<int64_t>(cur.b) * a.H + ((cur.block << heads_shift) + head_l) * group + row] = lse2 / paged::kLog2e;
+          } else {
+            a.part_lse[(slot0 + (first ? 0 : 1)) * n_rows + head_l * group + row] = lse2;
+          }
         }
       }
-    }
-    const int rows = group << heads_shift;
 #pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-      float* mine = merge + warp * 16 * S::kMergePitch;
+    for (int c32 = 0; c32 < D / 32; ++c32) {
+      float* mine = merge + warp * kHeadsOf * S::kMergePitch;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {   // (e4m3: the n-tiles of a unit are its even and its odd dims)
-          const int col = 2 * t4 + (x & 1);
-          const int dim = kE4M3 ? 16 * (i >> 1) + 2 * col + (i & 1) : 8 * i + col;
-          mine[(g4 + 8 * (x >> 1)) * S::kMergePitch + dim] = o[4 * c + i][x] * f[x >> 1];
-        }
-      __syncthreads();
-      for (int i = tid; i < rows * 16; i += 32 * kWarps) {   // two dims of a row
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int dim = kE4M3 ? 16 * i + 2 * g4 + (x >> 1) : 16 * i + g4 + 8 * (x >> 1);
+            mine[(8 * n + 2 * t4 + (x & 1)) * S::kMergePitch + dim] = o[n][2 * c32 + i][x] * f[n][x & 1];
+          }
+      workers_sync();
+      for (int i = tid; i < n_rows * 16; i += 32 * kWarps) {   // two dims of a head
         const int rr = i >> 4, d2 = 2 * (i & 15), hl = rr / group, row = rr - hl * group;
         float2 sum = make_float2(0.f, 0.f);
         for (int w = 0; w < n_strips; ++w) {
-          const float2 x = *reinterpret_cast<const float2*>(merge + (((hl << strip_shift) + w) * 16 + row) * S::kMergePitch + d2);
+          const float2 x = *reinterpret_cast<const float2*>(merge + (((hl << strip_shift) + w) * kHeadsOf + row) * S::kMergePitch + d2);
           sum.x += x.x;
           sum.y += x.y;
         }
-        const int h = ((cur.block << heads_shift) + hl) * group + row;
         if (from_start && to_end) {
-          uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + cur.b * a.ld_out + static_cast<int64_t>(h) * D + 32 * c + d2);
+          const int h = (cur.block << heads_shift) * group + rr;
+          uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + cur.b * a.ld_out + static_cast<int64_t>(h) * D + 32 * c32 + d2);
           *out = kF16 ? pack_f16(sum.x, sum.y) : pack_bf16(sum.x, sum.y);
         } else {
-          *reinterpret_cast<float2*>(a.part_out + ((slot0 + (first ? 0 : 1)) * rows + rr) * D + 32 * c + d2) = sum;
+          *reinterpret_cast<float2*>(a.part_out + ((slot0 + (first ? 0 : 1)) * n_rows + rr) * D + 32 * c32 + d2) = sum;
         }
       }
-      __syncthreads();
+      workers_sync();
     }
   };
 
-  fetch_pages();
-#pragma unroll
-  for (int i = 0; i < S::kStages - 1; ++i) copy(i);
-  begin();
-  bool from_start = first_is_start, first = true;
-  int stage = 0;
-  while (true) {
-    cp_async_wait<S::kStages - 2>();
-    __syncwarp();
-    work(stage);
-    __syncwarp();
-    copy(stage == 0 ? S::kStages - 1 : stage - 1);   // the stage of the strip before
-    stage = stage == S::kStages - 1 ? 0 : stage + 1;
-    const bool last_of_seq = cur.tile + 1 == cur.st.count;
-    if (cur.left == 1 && tid == 0) paged::say_parts(a, blockIdx.x, cur, from_start, first);
-    if (last_of_seq || cur.left == 1) {
-      finish(from_start, last_of_seq, first);
-      first = false;
-    }
-    const bool more = cur.left > 1;
-    const bool other = paged::advance(a, cur, shift, blocks);
-    if (!more) break;
-    if (other) {
-      begin();
-      from_start = true;
-    }
+  // sequences without tokens belong to no tile: their results, while the first tile is on its way
+  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
+    if (paged::seq_length(a, b, tid == 0) > 0) continue;
+    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + b * a.ld_out);
+    for (int i = tid; i < a.H * D / 8; i += 32 * kWarps) out[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < a.H && a.lse != nullptr; i += 32 * kWarps) a.lse[static_cast<int64_t>(b) * a.H + i] = -INFINITY;
   }
-  cp_async_wait<0>();
+  bool from_start = cur.tile == 0, first = true;
+  if (cur.left > 0) begin();
+  while (cur.left > 0) {
+    work();
+    const bool last_of_seq = cur.tile + 1 == cur.st.count;
+    if (!last_of_seq && cur.left > 1) {
+      ++cur.tile;
+      --cur.left;
+      continue;
+    }
+    if (cur.left == 1 && tid == 0) paged::say_parts(a, blockIdx.x, cur, from_start, first);
+    finish(from_start, last_of_seq, first);
+    first = false;
+    from_start = true;
+    paged::advance(a, cur, shift, blocks);
+    if (cur.left > 0) begin();
+  }
 }
 
 // ---- parts of a sequence that several units worked on -------------------------------------------------
@@ -558,7 +683,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(PagedAttnAr
 
 int heads_shift_of(int G) { return G % 8 == 0 ? 3 : G % 4 == 0 ? 2 : G % 2 == 0 ? 1 : 0; }
 
-static cudaError_t launch_paged_join(const PagedAttnArgs& a, int blocks, cudaStream_t st, int64_t* n_launch) {
+cudaError_t launch_paged_join(const PagedAttnArgs& a, int blocks, cudaStream_t st, int64_t* n_launch) {
   auto kernel = a.fp16 ? paged_join_kernel<__half> : paged_join_kernel<__nv_bfloat16>;
   cudaError_t e = launch_pdl(kernel, dim3(4 * a.units), dim3(32 * kJoinWarps), 0, st, a, a.H / blocks);
   if (e == cudaSuccess) e = cudaGetLastError();
@@ -566,24 +691,35 @@ static cudaError_t launch_paged_join(const PagedAttnArgs& a, int blocks, cudaStr
   return e;
 }
 
-template <typename T, int D, bool kE4M3>
+template <typename T, int D, bool kE4M3, int kTiles>
 cudaError_t launch_t(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
-  using S = Strip<D, kE4M3>;
+  using S = Shape<D, kE4M3, kTiles>;
   static_assert(S::kSmem <= 227 * 1024, "shared memory of a block");
-  auto kernel = paged_attn_kernel<T, D, kE4M3>;
+  const uint64_t rows = static_cast<uint64_t>(a.n_pages > 0 ? a.n_pages : 1) << a.page_shift;
+  const int hs = heads_shift_of(a.G), tile_keys = S::kRows << (3 - hs);
+  const uint32_t box_rows = (1 << a.page_shift) < tile_keys ? 1 << a.page_shift : tile_keys;
+  CUtensorMap k_map, v_map;
+  const bool ok = kE4M3 ? make_map_u8_blocks(&k_map, a.k_pool, D, a.G, rows, a.ld_k, box_rows, 1 << hs) && make_map_u8_blocks(&v_map, a.v_pool, D, a.G, rows, a.ld_v, box_rows, 1 << hs)
+                        : make_map_16bit_blocks(&k_map, a.k_pool, a.G * D / 64, rows, a.ld_k, box_rows, S::kBlocks << hs) &&
+                              make_map_16bit_blocks(&v_map, a.v_pool, a.G * D / 64, rows, a.ld_v, box_rows, S::kBlocks << hs);
+  if (!ok) return cudaErrorInvalidValue;
+  auto kernel = paged_attn_kernel<T, D, kE4M3, kTiles>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
-  const int hs = heads_shift_of(a.G);
-  e = launch_pdl(kernel, dim3(a.units), dim3(32 * kWarps), S::kSmem, st, a, hs);
+  e = launch_pdl(kernel, dim3(a.units), dim3(kThreads), S::kSmem, st, k_map, v_map, a, hs);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   ++*n_launch;
   return launch_paged_join(a, a.G >> hs, st, n_launch);
 }
+template <typename T, int D, bool kE4M3>
+cudaError_t launch_n(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
+  return a.H / a.G <= 8 ? launch_t<T, D, kE4M3, 1>(a, st, n_launch) : launch_t<T, D, kE4M3, 2>(a, st, n_launch);
+}
 template <typename T>
 cudaError_t launch_d(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
-  if (a.d == 128) return a.e4m3 ? launch_t<T, 128, true>(a, st, n_launch) : launch_t<T, 128, false>(a, st, n_launch);
-  return a.e4m3 ? launch_t<T, 64, true>(a, st, n_launch) : launch_t<T, 64, false>(a, st, n_launch);
+  if (a.d == 128) return a.e4m3 ? launch_n<T, 128, true>(a, st, n_launch) : launch_n<T, 128, false>(a, st, n_launch);
+  return a.e4m3 ? launch_n<T, 64, true>(a, st, n_launch) : launch_n<T, 64, false>(a, st, n_launch);
 }
 
 }  // namespace
@@ -593,7 +729,6 @@ int64_t paged_entries(const PagedAttnArgs& a) {
   const int hs = heads_shift_of(a.G), keys = a.latent ? 64 : 16 << (3 - hs);   // (at least so many keys a tile)
   return static_cast<int64_t>(a.batch) * (a.max_len / keys + 2) * (a.G >> hs);
 }
-
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {
   return a.fp16 ? launch_d<__half>(a, st, n_launch) : launch_d<__nv_bfloat16>(a, st, n_launch);

@@ -381,6 +381,11 @@ bool make_map_bf16_rows(CUtensorMap* map, const void* base, uint64_t cols, uint6
 // A bf16 matrix [rows, ld] seen as [n_blocks of 64 columns][rows][64 columns]: one box (coordinates 0, row, 0) brings
 // box_rows rows x n_blocks column blocks, each block a 128-byte swizzled tile of its own, block after block.
 bool make_map_bf16_tile(CUtensorMap* map, const void* base, uint64_t ld, uint64_t rows, uint32_t box_rows, uint32_t n_blocks);
+// Rows of 16-bit elements `ld` apart, as blocks of 64 columns (n_all of them); one box (coordinates 0, row, block) brings box_rows rows x
+// n_box blocks, block after block, 128-byte swizzled.
+bool make_map_16bit_blocks(CUtensorMap* map, const void* base, uint64_t n_all, uint64_t rows, uint64_t ld, uint32_t box_rows, uint32_t n_box);
+// The same of bytes, blocks of `cols` (64 or 128) columns, swizzled over 64 or 128 bytes.
+bool make_map_u8_blocks(CUtensorMap* map, const void* base, uint32_t cols, uint64_t n_all, uint64_t rows, uint64_t ld, uint32_t box_rows, uint32_t n_box);
 // 16-bit rows of `cols` (a multiple of 64) elements, `rows` of them in each of `groups` groups `ld` elements apart, seen as
 // [group][block of 64 columns][row][64 columns]: one box (coordinates 0, row, 0, group) brings box_rows rows x all column blocks, each block
 // a 128-byte swizzled tile of its own; rows past a group's last are zeros.
