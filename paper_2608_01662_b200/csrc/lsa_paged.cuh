@@ -42,9 +42,9 @@ __device__ __forceinline__ int seq_length(const PagedAttnArgs& a, int b, bool re
   return n;
 }
 
-__device__ __forceinline__ SeqTiles seq_tiles(const PagedAttnArgs& a, int b, int shift) {
+__device__ __forceinline__ SeqTiles tiles_of(const PagedAttnArgs& a, int n, int shift) {
   SeqTiles t;
-  t.n = seq_length(a, b);
+  t.n = n;
   const int all = (t.n + (1 << shift) - 1) >> shift;
   if (a.window <= 0 || t.n <= static_cast<int64_t>(a.sink) + a.window) {
     t.lo = t.sink = t.head = t.skip = 0;
@@ -60,6 +60,8 @@ __device__ __forceinline__ SeqTiles seq_tiles(const PagedAttnArgs& a, int b, int
   return t;
 }
 
+__device__ __forceinline__ SeqTiles seq_tiles(const PagedAttnArgs& a, int b, int shift) { return tiles_of(a, seq_length(a, b), shift); }
+
 // Where a unit is in the list.
 struct Cursor {
   int b, block, tile;   // sequence, block of KV heads, tile
@@ -71,10 +73,13 @@ struct Cursor {
 // entries: the host sees to that.)
 __device__ __forceinline__ Cursor first_entry(const PagedAttnArgs& a, int unit, int shift, int blocks, int lane) {
   const int run = (a.batch + 31) / 32;
-  int mine = 0;
+  int mine = 0, n = 0;
   for (int i = 0; i < run; ++i) {
     const int b = lane * run + i;
-    if (b < a.batch) mine += seq_tiles(a, b, shift).count;
+    if (b < a.batch) {
+      n = seq_length(a, b);
+      mine += tiles_of(a, n, shift).count;
+    }
   }
   mine *= blocks;
   int upto = mine;   // inclusive scan
@@ -92,10 +97,14 @@ __device__ __forceinline__ Cursor first_entry(const PagedAttnArgs& a, int unit, 
   const int owner = __ffs(__ballot_sync(0xffffffffu, upto > t0)) - 1;
   int off = static_cast<int>(t0) - __shfl_sync(0xffffffffu, upto - mine, owner);
   c.b = owner * run;
-  c.st = seq_tiles(a, c.b, shift);
-  while (c.st.count * blocks <= off) {
-    off -= c.st.count * blocks;
-    c.st = seq_tiles(a, ++c.b, shift);
+  if (run == 1) {   // (the owner has the length: a load less on the way to the first tile)
+    c.st = tiles_of(a, __shfl_sync(0xffffffffu, n, owner), shift);
+  } else {
+    c.st = seq_tiles(a, c.b, shift);
+    while (c.st.count * blocks <= off) {
+      off -= c.st.count * blocks;
+      c.st = seq_tiles(a, ++c.b, shift);
+    }
   }
   while (off >= c.st.count) {   // (`blocks` is small)
     off -= c.st.count;
@@ -126,6 +135,54 @@ __device__ __forceinline__ void say_parts(const PagedAttnArgs& a, int unit, cons
   const int rest = last.st.count - (last.tile + 1);
   const bool goes_on = begins_here && rest > 0;
   a.parts[unit] = make_int4(goes_on ? 1 + (rest + last.per - 1) / last.per : 0, last.b, last.block, 2 * unit + (first ? 0 : 1));
+}
+
+// ---- the kernels that join parts: what a block has to do.
+// The units' words about their parts give each owner (a unit that holds a beginning) a number of rounds; round `it` of all of them is
+// looked up by the threads together.
+constexpr int kJoinThreads = 256;
+struct JoinList {
+  int warp_sum[kJoinThreads / 32];
+  int4 own;        // of the round at hand: {parts, sequence, block, slot of the first part}
+  int unit, round;
+};
+// By all kJoinThreads threads.  rounds_of(parts): rounds of an owner.  begins: rounds before this thread's unit; returns all rounds.
+template <class F>
+__device__ __forceinline__ int join_list(const PagedAttnArgs& a, JoinList& s, int tid, int4* mine, int* begins, F rounds_of) {
+  static_assert(kMaxPagedUnits <= kJoinThreads, "a thread per unit");
+  const int lane = tid & 31, warp = tid >> 5;
+  *mine = tid < a.units ? __ldcg(a.parts + tid) : make_int4(0, 0, 0, 0);
+  // (units that gave up on a wait have left nothing, and nothing said about it)
+  const bool raised = a.status != nullptr && *reinterpret_cast<const volatile int*>(a.status) != 0;
+  const int x = rounds_of(mine->x);
+  int upto = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
+  }
+  if (lane == 31) s.warp_sum[warp] = upto;
+  if (__syncthreads_or(raised)) return 0;
+  int before = 0, total = 0;
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / 32; ++i) {
+    const int w = s.warp_sum[i];
+    if (i < warp) before += w;
+    total += w;
+  }
+  *begins = before + upto - x;
+  return total;
+}
+// The owner of round `it`, for all threads (it < all rounds).
+template <class F>
+__device__ __forceinline__ void join_find(JoinList& s, int tid, int it, const int4& mine, int begins, F rounds_of) {
+  __syncthreads();   // (the round before has been worked on)
+  if (it >= begins && it < begins + rounds_of(mine.x)) {
+    s.own = mine;
+    s.unit = tid;
+    s.round = it - begins;
+  }
+  __syncthreads();
 }
 
 }  // namespace paged

@@ -460,6 +460,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   // ---- end of a (sequence, block) for this unit: the strips' parts are put together, 32 dims at a time
   const int64_t slot0 = 2 * static_cast<int64_t>(blockIdx.x);
   const int n_rows = group << heads_shift;
+  const int group_inv = 65536 / group + 1;   // (row * group_inv) >> 16 is row / group for rows below 128
   auto finish = [&](bool from_start, bool to_end, bool first) {
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
@@ -476,11 +477,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const int row = 8 * n + 2 * t4 + c;
-        float m = -INFINITY, l = 0.f;
-        const float2* all = ml + (head_l << strip_shift) * kHeadsOf + row;
-        for (int w = 0; w < n_strips; ++w) m = fmaxf(m, all[kHeadsOf * w].x);
+        // (each of the eight lanes of a head looks at one strip)
+        const float2 mine = g4 < n_strips ? ml[((head_l << strip_shift) + g4) * kHeadsOf + row] : make_float2(-INFINITY, 0.f);
+        float m = mine.x;
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
         const float ref = m > -INFINITY ? m : 0.f;
-        for (int w = 0; w < n_strips; ++w) l += all[kHeadsOf * w].y * exp2_fast(all[kHeadsOf * w].x - ref);
+        float l = mine.y * exp2_fast(mine.x - ref);
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
         const bool some = l > 0.f || l != l;
         f[n][c] = some ? exp2_fast(m_used[n][c] - ref) / l : 0.f;
         if (strip == 0 && g4 == 0 && row < group) {
@@ -506,12 +511,17 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           }
       workers_sync();
       for (int i = tid; i < n_rows * 16; i += 32 * kWarps) {   // two dims of a head
-        const int rr = i >> 4, d2 = 2 * (i & 15), hl = rr / group, row = rr - hl * group;
-        float2 sum = make_float2(0.f, 0.f);
-        for (int w = 0; w < n_strips; ++w) {
-          const float2 x = *reinterpret_cast<const float2*>(merge + (((hl << strip_shift) + w) * kHeadsOf + row) * S::kMergePitch + d2);
-          sum.x += x.x;
-          sum.y += x.y;
+        const int rr = i >> 4, d2 = 2 * (i & 15), hl = (rr * group_inv) >> 16, row = rr - hl * group;
+        const float* src = merge + ((hl << strip_shift) * kHeadsOf + row) * S::kMergePitch + d2;
+        float2 part[kWarps];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+          part[w] = w < n_strips ? *reinterpret_cast<const float2*>(src + w * kHeadsOf * S::kMergePitch) : make_float2(0.f, 0.f);
+        float2 sum = part[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) {
+          sum.x += part[w].x;
+          sum.y += part[w].y;
         }
         if (from_start && to_end) {
           const int h = (cur.block << heads_shift) * group + rr;
@@ -564,42 +574,22 @@ __device__ __forceinline__ void store4(T* out, const float4& x) {
 }
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(PagedAttnArgs a, int rows) {
-  __shared__ int4 parts[kMaxPagedUnits];
-  __shared__ int upto[kMaxPagedUnits];     // rounds of a block for the owners up to this one
+  static_assert(paged::kJoinThreads == 32 * kJoinWarps, "threads of a block");
+  __shared__ paged::JoinList list;
   __shared__ float4 acc[kJoinWarps][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
-  for (int i = tid; i < a.units; i += 32 * kJoinWarps) parts[i] = __ldcg(a.parts + i);
-  // (units that gave up on a wait have left nothing, and nothing said about it)
-  if (__syncthreads_or(a.status != nullptr && *reinterpret_cast<const volatile int*>(a.status) != 0)) return;
   const int chunks = max(a.dv / kManyDims, 1), chunk_dims = min(a.dv, kManyDims);
-  auto rounds = [&](int n) { return n == 0 ? 0 : n <= kFewParts ? (rows + kJoinWarps - 1) / kJoinWarps : rows * chunks; };
-  if (warp == 0) {
-    int sum = 0;
-    for (int i0 = 0; i0 < a.units; i0 += 32) {
-      int x = i0 + lane < a.units ? rounds(parts[i0 + lane].x) : 0;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      if (i0 + lane < a.units) upto[i0 + lane] = sum + x;
-      sum += __shfl_sync(0xffffffffu, x, 31);
-    }
-  }
-  __syncthreads();
-  const int total = upto[a.units - 1];
+  auto rounds_of = [&](int n) { return n == 0 ? 0 : n <= kFewParts ? (rows + kJoinWarps - 1) / kJoinWarps : rows * chunks; };
+  int4 mine;
+  int begins;
+  const int total = paged::join_list(a, list, tid, &mine, &begins, rounds_of);
   for (int it = blockIdx.x; it < total; it += gridDim.x) {   // block-uniform
-    int lo = 0, hi = a.units - 1;   // the first owner with upto > it
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (upto[mid] > it) hi = mid;
-      else lo = mid + 1;
-    }
-    const int4 own = parts[lo];
-    const int n = own.x, round = it - (lo > 0 ? upto[lo - 1] : 0);
-    auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (lo + i); };
+    paged::join_find(list, tid, it, mine, begins, rounds_of);
+    const int4 own = list.own;
+    const int n = own.x, round = list.round, unit = list.unit;
+    auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (unit + i); };
     // the weights of the parts of a row, a lane's being those of parts lane, lane + 32, ...
     constexpr int kMine = (kMaxPagedUnits + 31) / 32;
     auto weights = [&](int row, float (&w)[kMine], float* lse) {
@@ -628,23 +618,24 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(PagedAttnAr
     };
     float w[kMine], lse;
     if (n <= kFewParts) {
-      const int row = round * kJoinWarps + warp;
+      const int row = round * kJoinWarps + warp, d = 4 * lane;
       if (row < rows) {   // whole warps
+        float4 y[kFewParts];   // (asked for before the weights are known: one trip to L2; a row has 64 or 128 dims)
+#pragma unroll
+        for (int i = 0; i < kFewParts; ++i)
+          if (i < n && d < a.dv) y[i] = __ldcg(reinterpret_cast<const float4*>(a.part_out + (slot(i) * rows + row) * a.dv + d));
         weights(row, w, &lse);
         const int h = own.z * rows + row;
         if (lane == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(own.y) * a.H + h] = lse;
-        for (int d = 4 * lane; d < a.dv; d += 128) {
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-          for (int i = 0; i < kFewParts; ++i) {
-            if (i < n) {
-              const float4 y = __ldcg(reinterpret_cast<const float4*>(a.part_out + (slot(i) * rows + row) * a.dv + d));
-              const float wi = __shfl_sync(__activemask(), w[0], i);
-              x.x += wi * y.x; x.y += wi * y.y; x.z += wi * y.z; x.w += wi * y.w;
-            }
+        for (int i = 0; i < kFewParts; ++i) {
+          const float wi = __shfl_sync(0xffffffffu, w[0], i);
+          if (i < n && d < a.dv) {
+            x.x += wi * y[i].x; x.y += wi * y[i].y; x.z += wi * y[i].z; x.w += wi * y[i].w;
           }
-          store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d, x);
         }
+        if (d < a.dv) store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d, x);
       }
     } else {
       const int row = round / chunks, d0 = (round - row * chunks) * chunk_dims;
@@ -666,7 +657,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(PagedAttnAr
           }
         }
       }
-      __syncthreads();   // (the round before has been read)
       acc[warp][lane] = x;
       __syncthreads();
       if (warp == 0) {

@@ -525,46 +525,24 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
 // Weights 2^(lse_i - max) / sum over the parts, a fixed order of addition.  A part is [dim][64 heads], so a thread has one head.  A
 // round of a block: few parts: 64 dims, 16 of them per thread; many (one long sequence is 148 parts of 128 KB, which all SMs have to
 // fetch together): two dims, four threads sharing the parts of a head.
-constexpr int kJoinThreads = 256, kFewParts = 8, kFewDims = 64, kManyDims = 2, kWays = 4;
+constexpr int kJoinThreads = paged::kJoinThreads, kFewParts = 8, kFewDims = 64, kManyDims = 2, kWays = 4;
 template <bool kF16>
 __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAttnArgs a) {
-  __shared__ int4 parts[kMaxPagedUnits];
-  __shared__ int upto[kMaxPagedUnits];     // rounds of a block for the owners up to this one
+  __shared__ paged::JoinList list;
   __shared__ uint32_t tile[kHeads][kFewDims / 2 + 1];
   __shared__ float red[kWays][kHeads][2];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int head = tid & 63, way = tid >> 6;
+  const int tid = threadIdx.x, head = tid & 63, way = tid >> 6;
   pdl_wait();
   pdl_launch_dependents();
-  for (int i = tid; i < a.units; i += kJoinThreads) parts[i] = __ldcg(a.parts + i);
-  // (units that gave up on a wait have left nothing, and nothing said about it)
-  if (__syncthreads_or(tc::status_raised(a.status))) return;
-  if (warp == 0) {
-    int sum = 0;
-    for (int i0 = 0; i0 < a.units; i0 += 32) {
-      const int n = i0 + lane < a.units ? parts[i0 + lane].x : 0;
-      int x = n == 0 ? 0 : n <= kFewParts ? kDV / kFewDims : kDV / kManyDims;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-      }
-      if (i0 + lane < a.units) upto[i0 + lane] = sum + x;
-      sum += __shfl_sync(0xffffffffu, x, 31);
-    }
-  }
-  __syncthreads();
-  const int total = upto[a.units - 1];
+  auto rounds_of = [](int n) { return n == 0 ? 0 : n <= kFewParts ? kDV / kFewDims : kDV / kManyDims; };
+  int4 mine;
+  int begins;
+  const int total = paged::join_list(a, list, tid, &mine, &begins, rounds_of);
   for (int it = blockIdx.x; it < total; it += gridDim.x) {   // block-uniform
-    int lo = 0, hi = a.units - 1;   // the first owner with upto > it
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (upto[mid] > it) hi = mid;
-      else lo = mid + 1;
-    }
-    const int4 own = parts[lo];
-    const int n = own.x, round = it - (lo > 0 ? upto[lo - 1] : 0);
-    auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (lo + i); };
+    paged::join_find(list, tid, it, mine, begins, rounds_of);
+    const int4 own = list.own;
+    const int n = own.x, round = list.round, unit = list.unit;
+    auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (unit + i); };
     uint16_t* out = static_cast<uint16_t*>(a.out) + own.y * a.ld_out;
     auto finish = [&](float m, float den) -> float {   // 1 / sum; the log-sum-exp of the head by one thread
       const bool some = den > 0.f || den != den;
@@ -597,7 +575,6 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
           for (int j = 0; j < kMine; ++j) x[j] += wi * __ldcg(src + j * kHeads);
         }
       }
-      __syncthreads();   // (the round before has been written out)
 #pragma unroll
       for (int j = 0; j < kMine; j += 2) tile[head][(way * kMine + j) / 2] = pack2<kF16>(x[j], x[j + 1]);
       __syncthreads();
@@ -609,7 +586,6 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
       float m = -INFINITY, den = 0.f;
       const float* lse = a.part_lse + head;
       for (int i = way; i < n; i += kWays) m = fmaxf(m, __ldcg(lse + slot(i) * kHeads));
-      __syncthreads();
       red[way][head][0] = m;
       __syncthreads();
 #pragma unroll
