@@ -166,19 +166,21 @@ def _kv_rows(t, width: int, dtype, where: str, rows: int | None = None):
     """(pointer, elements from one row to the next) of rows of `width` elements, given as [rows, width] or [rows, heads, dims]."""
     if t is None:
         return None, 0
+    n = t.size(0)
+    if t.dtype is dtype and t.is_contiguous() and t.numel() == n * width and (rows is None or n == rows):   # (most calls end here)
+        return t.data_ptr(), width
     st, sh = t.stride(), t.shape
-    n = len(sh)
-    inner = n >= 2 and st[-1] == 1 and (n == 2 or (n == 3 and (sh[1] == 1 or st[1] == sh[2])))
-    if not inner or t.dtype != dtype or (sh[1] if n == 2 else sh[1] * sh[2]) != width or (rows is not None and sh[0] != rows):
+    inner = len(sh) >= 2 and st[-1] == 1 and (len(sh) == 2 or (len(sh) == 3 and (sh[1] == 1 or st[1] == sh[2])))
+    if not inner or t.dtype is not dtype or (sh[1] if len(sh) == 2 else sh[1] * sh[2]) != width or (rows is not None and n != rows):
         raise LsaError(-1, where, f"rows of {width} {dtype} wanted{'' if rows is None else f', {rows} of them'}: got {tuple(sh)} {t.dtype}, strides {st}")
-    return t.data_ptr(), (st[0] if sh[0] > 1 else max(st[0], width))
+    return t.data_ptr(), (st[0] if n > 1 else max(st[0], width))
 
 
-def _kv_flat(t, dtype, count: int, where: str, exact: bool = True):
-    """Pointer to a contiguous array of `count` elements (or at least as many)."""
+def _kv_flat(t, dtype, count: int, where: str):
+    """Pointer to a contiguous array of `count` elements."""
     if t is None:
         return None
-    if t.dtype != dtype or not t.is_contiguous() or (t.numel() != count if exact else t.numel() < count):
+    if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
         raise LsaError(-1, where, f"{count} contiguous {dtype} wanted: got {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
 
@@ -214,14 +216,17 @@ class Context:
     def __init__(self, params: LsaParams | None, n_query: int, n_key_max: int, batch: int = 1, device=None, stream=None,
                  kv: LsaKvParams | None = None):
         """params: the sparse path's (None: the context serves kv_append and paged_attn only); kv: those calls' parameters."""
-        self.params = params
-        self.kv = kv
+        self.params, self.kv = params, kv
         self.device = torch.device(device if device is not None else "cuda:0")
         nbytes = workspace_bytes(params, n_query, n_key_max, batch) if params is not None or kv is None else 0
         if kv is not None:
             nbytes = max(nbytes, kv_workspace_bytes(kv))
-            self._kv_ref = ctypes.byref(kv)
+            # what every call needs of them (an attribute of a ctypes structure costs more than one of an object)
+            self._kv_ref, self._kv_page, self._kv_rope = ctypes.byref(kv), kv.kv_page, kv.d_rope
             self._kv_dtype = tuple(_KV_DTYPES.values())[kv.dtype]
+            self._kv_codes = {torch.float8_e4m3fn: torch.float8_e4m3fn} if kv.cache_e4m3 else None   # (else bytes)
+            self._kv_wk, self._kv_wv = kv.n_kv_heads * kv.d_qk, kv.n_kv_heads * kv.d_v
+            self._kv_wq, self._kv_wo = kv.n_heads * kv.d_qk, kv.n_heads * kv.d_v
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         h = c_void_p()
@@ -333,40 +338,41 @@ class Context:
 
     def _kv_cache(self, k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where):
         """The arguments of a cache: pools as [rows, heads * dims] or [rows, heads, dims], scales as [rows, heads]."""
-        kv = self.kv
-        if kv is None:
+        if self.kv is None:
             raise LsaError(-1, where, "the context was made without kv parameters")
-        rows, batch = k_pool.shape[0], page_table.shape[0]
-        dtype = k_pool.dtype if kv.cache_e4m3 and k_pool.dtype in (torch.uint8, torch.float8_e4m3fn) else torch.uint8 if kv.cache_e4m3 else self._kv_dtype
-        if rows % kv.kv_page:
-            raise LsaError(-1, where, f"a pool of {rows} rows is not a whole number of pages of {kv.kv_page}")
-        if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.stride(1) != 1:
+        rows, batch = k_pool.size(0), page_table.size(0)
+        n_pages, rest = divmod(rows, self._kv_page)
+        if rest:
+            raise LsaError(-1, where, f"a pool of {rows} rows is not a whole number of pages of {self._kv_page}")
+        if page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.stride(1) != 1:
             raise LsaError(-1, where, "page_table: int32 [batch, pages] with contiguous rows wanted")
-        return (*_kv_rows(k_pool, kv.n_kv_heads * kv.d_qk, dtype, where), *_kv_rows(v_pool, kv.n_kv_heads * kv.d_v, dtype, where, rows),
-                _kv_flat(k_scale, torch.float32, rows * kv.n_kv_heads, where), _kv_flat(v_scale, torch.float32, rows * kv.n_kv_heads, where),
-                rows // kv.kv_page, page_table.data_ptr(), page_table.stride(0) if batch > 1 else page_table.shape[1],
+        cached = self._kv_codes.get(k_pool.dtype, torch.uint8) if self._kv_codes else self._kv_dtype
+        k, ld_k = _kv_rows(k_pool, self._kv_wk, cached, where)
+        v, ld_v = _kv_rows(v_pool, self._kv_wv, cached, where, rows)
+        ks, vs = (None, None) if k_scale is None and v_scale is None else (_kv_flat(x, torch.float32, rows * self.kv.n_kv_heads, where) for x in (k_scale, v_scale))
+        return (k, ld_k, v, ld_v, ks, vs, n_pages, page_table.data_ptr(), page_table.stride(0) if batch > 1 else page_table.size(1),
                 _kv_flat(ctx_len, torch.int32, batch, where), batch)
 
     def kv_append(self, k_new, v_new, k_pool, v_pool, page_table, ctx_len, ctx_len_out=None, tok_start=None, q=None, q_out=None,
                   cos_sin=None, k_scale=None, v_scale=None):
         """lsa_kv_append: new tokens [n_tok, heads, dims] into the cache, rotated; q (optional) rotated into q_out."""
-        cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, "lsa_kv_append")
-        kv, batch = self.kv, cache[-1]
-        n_tok = k_new.shape[0]
-        if cos_sin is not None and (cos_sin.dim() != 2 or cos_sin.shape[1] != kv.d_rope):
-            raise LsaError(-1, "lsa_kv_append", f"cos_sin: [positions, {kv.d_rope}] wanted, got {tuple(cos_sin.shape)}")
+        where = "lsa_kv_append"
+        cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where)
+        batch, n_tok, n_pos, dtype = cache[-1], k_new.size(0), 0, self._kv_dtype
+        if cos_sin is not None:
+            n_pos = cos_sin.size(0)
+            if cos_sin.dim() != 2 or cos_sin.size(1) != self._kv_rope:
+                raise LsaError(-1, where, f"cos_sin: [positions, {self._kv_rope}] wanted, got {tuple(cos_sin.shape)}")
         self._chk(lib().lsa_kv_append(
-            self.h, self._kv_ref, *_kv_rows(k_new, kv.n_kv_heads * kv.d_qk, self._kv_dtype, "k_new"),
-            *_kv_rows(v_new, kv.n_kv_heads * kv.d_v, self._kv_dtype, "v_new", n_tok),
-            *_kv_rows(q, kv.n_heads * kv.d_qk, self._kv_dtype, "q", n_tok), *_kv_rows(q_out, kv.n_heads * kv.d_qk, self._kv_dtype, "q_out", n_tok),
-            n_tok, _kv_flat(tok_start, torch.int32, batch + 1, "tok_start"),
-            _kv_flat(cos_sin, torch.float32, 0 if cos_sin is None else cos_sin.numel(), "cos_sin"), 0 if cos_sin is None else cos_sin.shape[0],
-            *cache, _kv_flat(ctx_len_out, torch.int32, batch, "ctx_len_out")), "lsa_kv_append")
+            self.h, self._kv_ref, *_kv_rows(k_new, self._kv_wk, dtype, "k_new"), *_kv_rows(v_new, self._kv_wv, dtype, "v_new", n_tok),
+            *_kv_rows(q, self._kv_wq, dtype, "q", n_tok), *_kv_rows(q_out, self._kv_wq, dtype, "q_out", n_tok), n_tok,
+            _kv_flat(tok_start, torch.int32, batch + 1, "tok_start"), _kv_flat(cos_sin, torch.float32, n_pos * self._kv_rope, "cos_sin"), n_pos,
+            *cache, _kv_flat(ctx_len_out, torch.int32, batch, "ctx_len_out")), where)
 
     def paged_attn(self, q, k_pool, v_pool, page_table, ctx_len, out, lse=None, k_scale=None, v_scale=None):
         """lsa_paged_attn: q [batch, heads, d_qk] over each sequence's cached tokens -> out [batch, heads, d_v], lse [batch, heads]."""
-        cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, "lsa_paged_attn")
-        kv, batch = self.kv, cache[-1]
-        out_ptr, ld_out = _kv_rows(out, kv.n_heads * kv.d_v, self._kv_dtype, "out", batch)
-        self._chk(lib().lsa_paged_attn(self.h, self._kv_ref, *_kv_rows(q, kv.n_heads * kv.d_qk, self._kv_dtype, "q", batch), *cache, out_ptr, ld_out,
-                                       _kv_flat(lse, torch.float32, batch * kv.n_heads, "lse")), "lsa_paged_attn")
+        where = "lsa_paged_attn"
+        cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where)
+        batch, dtype = cache[-1], self._kv_dtype
+        self._chk(lib().lsa_paged_attn(self.h, self._kv_ref, *_kv_rows(q, self._kv_wq, dtype, "q", batch), *cache,
+                                       *_kv_rows(out, self._kv_wo, dtype, "out", batch), _kv_flat(lse, torch.float32, batch * self.kv.n_heads, "lse")), where)

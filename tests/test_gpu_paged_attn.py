@@ -230,10 +230,10 @@ def test_another_stream_and_a_captured_graph(cuda_device):
 def test_small_workspace_is_refused(cuda_device):
     c = pu.Cache([10], (8, 2, 64, 64), 16, "bf16", False, cuda_device, seed=17)
     small = binding.Context(None, 0, 0, 1, device=cuda_device, kv=binding.make_kv_params(1, 1, 64, 64, 16))
-    small.kv = c.params()
-    small._kv_ref = binding.ctypes.byref(small.kv)
+    large = binding.Context(None, 0, 0, 1, device=cuda_device, kv=c.params())
+    large.h, small.h = small.h, large.h       # the parameters of one, the workspace of the other
     with pytest.raises(binding.LsaError) as e:
-        pu.attend(c, small)
+        pu.attend(c, large)
     assert e.value.code == -3
 
 
