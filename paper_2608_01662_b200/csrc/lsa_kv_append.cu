@@ -42,15 +42,23 @@ template <typename T>
 __device__ __forceinline__ uint4 pack8(const float* x) {
   return make_uint4(Two<T>::put(x[0], x[1]), Two<T>::put(x[2], x[3]), Two<T>::put(x[4], x[5]), Two<T>::put(x[6], x[7]));
 }
-// Eight codes of value / scale: round to nearest even, saturating.
-__device__ __forceinline__ uint2 codes8(const float* x, float scale) {
+// Eight codes of value / scale: round to nearest even, saturating.  inv is 1 / scale, correctly rounded; q = x inv, then q + (x - q scale) inv
+// with the remainder in one fma is then the correctly rounded quotient (Markstein 1990), a third of the instructions of a division
+// each.  (A quotient too small for that to hold is far below the smallest code.)
+__device__ __forceinline__ uint2 codes8(const float* x, float scale, float inv) {
   uint32_t w[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t r = 0;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const float2 v = make_float2(__fdiv_rn(x[4 * h + 2 * j], scale), __fdiv_rn(x[4 * h + 2 * j + 1], scale));
+      float2 v = make_float2(x[4 * h + 2 * j], x[4 * h + 2 * j + 1]);
+      if (inv >= 1.17549435e-38f && inv < INFINITY) {
+        const float p = v.x * inv, q = v.y * inv;
+        v = make_float2(fmaf(fmaf(-p, scale, v.x), inv, p), fmaf(fmaf(-q, scale, v.y), inv, q));
+      } else {   // the reciprocal is not a normal number: a scale near either end of fp32, infinite or NaN
+        v = make_float2(__fdiv_rn(v.x, scale), __fdiv_rn(v.y, scale));
+      }
       r |= static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3)) << (16 * j);
     }
     w[h] = r;
@@ -65,22 +73,23 @@ __device__ __forceinline__ int32_t new_length(const KvAppendArgs& a, int i) {
   return a.ctx_len[i] + max(t1 - t0, 0);
 }
 
-constexpr int kRowsInFlight = 4;
-// Threads of a block: few tokens get a block that has all rows of 64 heads of 576 dims in flight at once; of many tokens several
-// share an SM.
+constexpr int kQAtOnce = 4, kKvAtOnce = 2;   // rows that a thread has on their way
+// Threads of a block: few tokens get a block that has all rows of 64 heads on their way at once; of many tokens several share an
+// SM, and a thread has enough rows to be worth the look-up of the token's place.
 template <int D>
 constexpr int kFewTokens = D == 576 ? 576 : 512;
 template <int D>
 constexpr int kManyTokens = D == 576 ? 288 : 64;
 
-// D: dims of a query or key head (and of a value head, if there are any).  Blocks are a multiple of 32 and of D / 16 threads.
-template <typename T, int D, bool kE4M3>
-__global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a) {
-  constexpr int kPlaces = D / 16;   // threads of a row
+// D: dims of a query or key head (and of a value head, if there are any).  kThreads: a multiple of 32 and of D / 16.
+template <typename T, int D, bool kE4M3, int kThreads>
+__global__ void __launch_bounds__(kThreads) kv_append_kernel(KvAppendArgs a) {
+  constexpr int kPlaces = D / 16, kRows = kThreads / kPlaces;   // threads of a row, rows of a block at a time
+  static_assert(kThreads % 32 == 0 && kThreads % kPlaces == 0, "whole rows");
   const int tid = threadIdx.x;
   const int64_t tok = blockIdx.x;
   // ---- the thread's place: vectors v0 and v1 (of eight elements) of every row it visits
-  const int place = tid % kPlaces, lane_row = tid / kPlaces, rows_at_once = blockDim.x / kPlaces;
+  const int place = tid % kPlaces, row0 = tid / kPlaces;
   const bool turns = 16 * place < a.d_rope;
   int v0, v1;
   if (turns) {
@@ -91,26 +100,29 @@ __global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a
     if (v0 >= a.rope_at / 8) v0 += a.d_rope / 8;
     v1 = v0 + 1;
   }
-  // rows of the token: query heads, key heads, value heads
-  const int n_q = a.q != nullptr ? a.H : 0, n_k = n_q + a.G, n_rows = a.latent ? n_k : n_k + a.G;
-  const bool in_place = a.q == a.q_out;
-  auto skipped = [&](int r) { return r >= n_rows || (r < n_q && in_place && !turns); };   // (what is not rotated in place stays)
-  uint4 u[kRowsInFlight][2];
-  auto fetch = [&](int r0) {
-#pragma unroll
-    for (int k = 0; k < kRowsInFlight; ++k) {
-      const int r = r0 + k * rows_at_once + lane_row;
-      if (skipped(r)) continue;
-      const T* src = r < n_q ? static_cast<const T*>(a.q) + tok * a.ld_q + r * D
-                     : r < n_k ? static_cast<const T*>(a.k_new) + tok * a.ld_k_new + (r - n_q) * D
-                               : static_cast<const T*>(a.v_new) + tok * a.ld_v_new + (r - n_k) * D;
-      u[k][0] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * v0));
-      u[k][1] = __ldcs(reinterpret_cast<const uint4*>(src + 8 * v1));
-    }
+  const int e0 = 8 * v0, e1 = 8 * (v1 - v0);
+  const int n_q = a.q != nullptr && (turns || a.q != a.q_out) ? a.H : 0;   // (what is not rotated in place stays)
+  const int n_kv = a.latent ? a.G : 2 * a.G;                               // key rows, then value rows
+  // (a row past the last is the last once more: no branches around loads; stores are guarded)
+  auto q_row = [&](int r) -> const T* { return static_cast<const T*>(a.q) + tok * a.ld_q + min(r, a.H - 1) * D + e0; };
+  auto kv_row = [&](int r) -> const T* {
+    r = min(r, n_kv - 1);
+    return (r < a.G ? static_cast<const T*>(a.k_new) + tok * a.ld_k_new + r * D : static_cast<const T*>(a.v_new) + tok * a.ld_v_new + (r - a.G) * D) + e0;
   };
+  auto load = [&](const T* p, uint4 (&u)[2]) {
+    u[0] = __ldcs(reinterpret_cast<const uint4*>(p));
+    u[1] = __ldcs(reinterpret_cast<const uint4*>(p + e1));
+  };
+  uint4 uq[kQAtOnce][2], ukv[kKvAtOnce][2];
   pdl_wait();
   pdl_launch_dependents();
-  fetch(0);   // the rows do not depend on where they go: they are on their way while that is looked up
+  // the rows do not depend on where they go: they are on their way while that is looked up
+  if (n_q > 0) {
+#pragma unroll
+    for (int k = 0; k < kQAtOnce; ++k) load(q_row(row0 + k * kRows), uq[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kKvAtOnce; ++k) load(kv_row(row0 + k * kRows), ukv[k]);
 
   // ---- the token's sequence, position and cache row (the same loads in every thread of the block)
   int b = static_cast<int>(tok);
@@ -141,75 +153,108 @@ __global__ void __launch_bounds__(kFewTokens<D>) kv_append_kernel(KvAppendArgs a
   if (mine && !fits && tid == 0) paged::report_index(a.notice);
 
   if (fits) {
-    float c[8], s[8];
+    float2 c[4], s[4];   // of the eight pairs
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      c[j] = make_float2(1.f, 1.f);
+      s[j] = make_float2(0.f, 0.f);
+    }
     if (turns) {
-      const float4* cs = reinterpret_cast<const float4*>(a.cos_sin + pos * a.d_rope + 8 * place);
-      const float4* sn = reinterpret_cast<const float4*>(a.cos_sin + pos * a.d_rope + a.d_rope / 2 + 8 * place);
+      const float* at = a.cos_sin + pos * a.d_rope + 8 * place;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float4 x = __ldg(cs + h), y = __ldg(sn + h);
-        c[4 * h] = x.x; c[4 * h + 1] = x.y; c[4 * h + 2] = x.z; c[4 * h + 3] = x.w;
-        s[4 * h] = y.x; s[4 * h + 1] = y.y; s[4 * h + 2] = y.z; s[4 * h + 3] = y.w;
+        const float4 x = __ldg(reinterpret_cast<const float4*>(at) + h), y = __ldg(reinterpret_cast<const float4*>(at + a.d_rope / 2) + h);
+        c[2 * h] = make_float2(x.x, x.y);
+        c[2 * h + 1] = make_float2(x.z, x.w);
+        s[2 * h] = make_float2(y.x, y.y);
+        s[2 * h + 1] = make_float2(y.z, y.w);
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) c[j] = 1.f, s[j] = 0.f;
     }
+    // x cos - y sin and y cos + x sin of the eight pairs of x[0 .. 15]
     auto turn = [&](float (&x)[16]) {
       if (a.interleaved) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float p = x[2 * j], q = x[2 * j + 1];
-          x[2 * j] = p * c[j] - q * s[j];
-          x[2 * j + 1] = q * c[j] + p * s[j];
+          const float p = x[2 * j], q = x[2 * j + 1], cc = j & 1 ? c[j / 2].y : c[j / 2].x, ss = j & 1 ? s[j / 2].y : s[j / 2].x;
+          x[2 * j] = p * cc - q * ss;
+          x[2 * j + 1] = q * cc + p * ss;
         }
       } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float p = x[j], q = x[j + 8];
-          x[j] = p * c[j] - q * s[j];
-          x[j + 8] = q * c[j] + p * s[j];
+        for (int j = 0; j < 4; ++j) {
+          const float2 p = make_float2(x[2 * j], x[2 * j + 1]), q = make_float2(x[8 + 2 * j], x[8 + 2 * j + 1]);
+          const float2 zero = make_float2(0.f, 0.f), minus = make_float2(-q.x, -q.y);
+          const float2 u = fma2(p, c[j], fma2(minus, s[j], zero)), v = fma2(q, c[j], fma2(p, s[j], zero));
+          x[2 * j] = u.x; x[2 * j + 1] = u.y;
+          x[8 + 2 * j] = v.x; x[8 + 2 * j + 1] = v.y;
         }
       }
     };
-    for (int r0 = 0; r0 < n_rows; r0 += kRowsInFlight * rows_at_once) {   // (the same trips for all lanes of a warp: the shuffles below)
-      if (r0 > 0) fetch(r0);
+    auto turned = [&](uint4 (&u)[2]) {
+      float x[16];
+      unpack8<T>(u[0], x);
+      unpack8<T>(u[1], x + 8);
+      turn(x);
+      u[0] = pack8<T>(x);
+      u[1] = pack8<T>(x + 8);
+    };
+
+    // ---- query heads
+    T* q_out = static_cast<T*>(a.q_out) + tok * a.ld_q_out + e0;
+    for (int r0 = row0; r0 < n_q; r0 += kQAtOnce * kRows) {
+      if (r0 != row0) {
 #pragma unroll
-      for (int k = 0; k < kRowsInFlight; ++k) {
-        const int r = r0 + k * rows_at_once + lane_row;
-        const bool on = !skipped(r), is_q = r < n_q, is_v = r >= n_k;
-        float x[16];
-        if (turns || kE4M3) {
-          unpack8<T>(u[k][0], x);
-          unpack8<T>(u[k][1], x + 8);
-          if (turns && !is_v) turn(x);
+        for (int k = 0; k < kQAtOnce; ++k) load(q_row(r0 + k * kRows), uq[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kQAtOnce; ++k) {
+        const int r = r0 + k * kRows;
+        if (turns) turned(uq[k]);
+        if (r < n_q) {
+          *reinterpret_cast<uint4*>(q_out + r * D) = uq[k][0];
+          *reinterpret_cast<uint4*>(q_out + r * D + e1) = uq[k][1];
         }
-        if (kE4M3 && r0 + (k + 1) * rows_at_once > n_q) {   // block-uniform: rows of the cache are among these
+      }
+    }
+
+    // ---- key heads, then value heads
+    for (int r0 = 0; r0 < n_kv; r0 += kKvAtOnce * kRows) {   // (the same trips for all lanes of a warp: the shuffles below)
+      if (r0 > 0) {
+#pragma unroll
+        for (int k = 0; k < kKvAtOnce; ++k) load(kv_row(r0 + row0 + k * kRows), ukv[k]);
+      }
+#pragma unroll
+      for (int k = 0; k < kKvAtOnce; ++k) {
+        const int r = r0 + row0 + k * kRows;
+        const bool on = r < n_kv, is_v = r >= a.G;
+        const int g = is_v ? r - a.G : r;
+        const int64_t at = row * (is_v ? a.ld_v : a.ld_k) + g * D + e0;
+        void* pool = is_v ? a.v_pool : a.k_pool;
+        if constexpr (kE4M3) {
+          float x[16];
+          unpack8<T>(ukv[k][0], x);
+          unpack8<T>(ukv[k][1], x + 8);
+          if (turns && !is_v) turn(x);
           float top = 0.f;
 #pragma unroll
           for (int j = 0; j < 16; ++j) top = fmaxf(top, fabsf(x[j]));
 #pragma unroll
           for (int o = kPlaces / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          if (on && !is_q) {
-            float scale = __fdiv_rn(top, 448.f);
-            if (scale == 0.f) scale = 1.f;   // (a zero row, or one so small that the quotient is)
-            const int g = is_v ? r - n_k : r - n_q;
-            uint8_t* dst = static_cast<uint8_t*>(is_v ? a.v_pool : a.k_pool) + row * (is_v ? a.ld_v : a.ld_k) + g * D;
-            *reinterpret_cast<uint2*>(dst + 8 * v0) = codes8(x, scale);
-            *reinterpret_cast<uint2*>(dst + 8 * v1) = codes8(x + 8, scale);
+          float scale = __fdiv_rn(top, 448.f);
+          if (scale == 0.f) scale = 1.f;   // (a zero row, or one so small that the quotient is)
+          const float inv = __frcp_rn(scale);
+          const uint2 lo = codes8(x, scale, inv), hi = codes8(x + 8, scale, inv);
+          if (on) {
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + at) = lo;
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(pool) + at + e1) = hi;
             if (place == 0) (is_v ? a.v_scale : a.k_scale)[row * a.G + g] = scale;
           }
-        }
-        if (on && (is_q || !kE4M3)) {
-          if (turns && !is_v) {
-            u[k][0] = pack8<T>(x);
-            u[k][1] = pack8<T>(x + 8);
+        } else {
+          if (turns && !is_v) turned(ukv[k]);
+          if (on) {
+            *reinterpret_cast<uint4*>(static_cast<T*>(pool) + at) = ukv[k][0];
+            *reinterpret_cast<uint4*>(static_cast<T*>(pool) + at + e1) = ukv[k][1];
           }
-          T* dst = is_q ? static_cast<T*>(a.q_out) + tok * a.ld_q_out + r * D
-                   : is_v ? static_cast<T*>(a.v_pool) + row * a.ld_v + (r - n_k) * D
-                          : static_cast<T*>(a.k_pool) + row * a.ld_k + (r - n_q) * D;
-          *reinterpret_cast<uint4*>(dst + 8 * v0) = u[k][0];
-          *reinterpret_cast<uint4*>(dst + 8 * v1) = u[k][1];
         }
       }
     }
@@ -236,8 +281,9 @@ __global__ void kv_lengths_kernel(KvAppendArgs a) {
 
 template <typename T, int D, bool kE4M3>
 cudaError_t launch_t(const KvAppendArgs& a, cudaStream_t st) {
-  const int threads = a.n_tok <= 2 * a.sm_count ? kFewTokens<D> : kManyTokens<D>;
-  return launch_pdl(kv_append_kernel<T, D, kE4M3>, dim3(static_cast<unsigned>(a.n_tok)), dim3(threads), 0, st, a);
+  const dim3 grid(static_cast<unsigned>(a.n_tok));
+  if (a.n_tok <= 2 * a.sm_count) return launch_pdl(kv_append_kernel<T, D, kE4M3, kFewTokens<D>>, grid, dim3(kFewTokens<D>), 0, st, a);
+  return launch_pdl(kv_append_kernel<T, D, kE4M3, kManyTokens<D>>, grid, dim3(kManyTokens<D>), 0, st, a);
 }
 template <typename T>
 cudaError_t launch_d(const KvAppendArgs& a, cudaStream_t st) {

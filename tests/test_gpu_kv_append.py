@@ -233,6 +233,30 @@ def test_tokens_that_do_not_fit_are_reported_and_skipped(cuda_device):
     run(lambda before: None)
 
 
+def test_e4m3_rows_with_infinities_nan_and_extreme_sizes(cuda_device):
+    """scale = amax / 448 over the numbers that are ones, code = value / scale: what fp32 division and the format give."""
+    n = 8
+    c, t, old = make((8, 2, 64, 64), [5] * n, [1] * n, 16, "bf16", True, cuda_device, True, 0, 0, False, seed=19)
+    t.v[0, 0, 3] = torch.inf
+    t.v[1, 0, 4] = torch.nan
+    t.v[2] = t.v[2].float() * 2.0 ** -124      # scales near the smallest numbers: their reciprocals overflow
+    t.v[3] = t.v[3].float() * 2.0 ** 126       # scales whose reciprocals are not normal numbers
+    t.v[4] = 0
+    t.v[5] = t.v[5].float() * 2.0 ** -132
+    t.v[6, 1] = -torch.inf
+    ctx = t.append()
+    assert ctx.status() == 0
+    x = t.v.float().cpu()
+    top = x.abs().nan_to_num(nan=0.0, posinf=torch.inf).amax(-1)
+    scale = torch.where(top / 448 == 0, torch.ones_like(top), top / 448)
+    want = (x / scale[..., None]).clamp(-448, 448).to(torch.float8_e4m3fn)
+    rows = [int(orc.paged_rows([4], c.table[b], 16)[0]) for b in range(n)]
+    got = c.v[rows].view(torch.float8_e4m3fn).reshape(n, 2, 64).cpu()
+    assert torch.equal(c.v_scale[rows].cpu(), scale)
+    assert torch.equal(got.float().isnan(), want.float().isnan())
+    assert torch.equal(got.float().nan_to_num(), want.float().nan_to_num())
+
+
 def test_token_starts_that_leave_the_tokens_are_reported(cuda_device):
     c, t, old = make((8, 2, 64, 64), [3, 20], [3, 4], 16, "bf16", False, cuda_device, False, 0, 0, False, seed=9)
     ctx = t.append()
