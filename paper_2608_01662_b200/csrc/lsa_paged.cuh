@@ -146,15 +146,16 @@ struct JoinList {
   int4 own;        // of the round at hand: {parts, sequence, block, slot of the first part}
   int unit, round;
 };
-// By all kJoinThreads threads.  rounds_of(parts): rounds of an owner.  begins: rounds before this thread's unit; returns all rounds.
+// By all kJoinThreads threads.  rounds_of(parts, owners): rounds of an owner.  begins: rounds before this thread's unit; returns all rounds.
 template <class F>
-__device__ __forceinline__ int join_list(const PagedAttnArgs& a, JoinList& s, int tid, int4* mine, int* begins, F rounds_of) {
+__device__ __forceinline__ int join_list(const PagedAttnArgs& a, JoinList& s, int tid, int4* mine, int* begins, int* owners, F rounds_of) {
   static_assert(kMaxPagedUnits <= kJoinThreads, "a thread per unit");
   const int lane = tid & 31, warp = tid >> 5;
   *mine = tid < a.units ? __ldcg(a.parts + tid) : make_int4(0, 0, 0, 0);
   // (units that gave up on a wait have left nothing, and nothing said about it)
   const bool raised = a.status != nullptr && *reinterpret_cast<const volatile int*>(a.status) != 0;
-  const int x = rounds_of(mine->x);
+  *owners = __syncthreads_count(mine->x > 0);
+  const int x = rounds_of(mine->x, *owners);
   int upto = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -175,9 +176,9 @@ __device__ __forceinline__ int join_list(const PagedAttnArgs& a, JoinList& s, in
 }
 // The owner of round `it`, for all threads (it < all rounds).
 template <class F>
-__device__ __forceinline__ void join_find(JoinList& s, int tid, int it, const int4& mine, int begins, F rounds_of) {
+__device__ __forceinline__ void join_find(JoinList& s, int tid, int it, const int4& mine, int begins, int owners, F rounds_of) {
   __syncthreads();   // (the round before has been worked on)
-  if (it >= begins && it < begins + rounds_of(mine.x)) {
+  if (it >= begins && it < begins + rounds_of(mine.x, owners)) {
     s.own = mine;
     s.unit = tid;
     s.round = it - begins;

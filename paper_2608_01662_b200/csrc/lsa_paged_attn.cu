@@ -38,7 +38,8 @@ struct Shape {
   static constexpr int kRows = kRowBytes == 256 ? 16 : 32, kRowShift = kRows == 32 ? 5 : 4;   // of a strip
   static constexpr int kBytes = kWarps * kRows * kRowBytes;        // of a tile's keys, and of its values: one slot each
   static constexpr int kScales = kE4M3 ? kWarps * kRows * 4 : 0;
-  static constexpr int kMergePitch = 34;                           // floats: 32 dims of a head and a gap
+  static constexpr int kMergeDims = kTiles == 2 ? 32 : 64;   // dims that are put together at a time: what there is room for
+  static constexpr int kMergePitch = kMergeDims + 2;               // floats
   static constexpr int kMerge = kWarps * 8 * kTiles * kMergePitch * 4;
   static constexpr int kSmem = 1024 + kRing * (kBytes + kScales) + kMerge + kWarps * 8 * kTiles * 8 + 2 * kRing * 8;
 };
@@ -497,41 +498,51 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           }
         }
       }
+    // With one strip a tile a warp has all of its head: it turns its rows by itself.
+    const bool alone = n_strips == 1;
+    auto meet = [&]() {
+      if (alone) __syncwarp();
+      else workers_sync();
+    };
+    const int i0 = alone ? lane : tid, step = alone ? 32 : 32 * kWarps, base_row = alone ? head_l * group : 0, my_rows = alone ? group : n_rows;
 #pragma unroll
-    for (int c32 = 0; c32 < D / 32; ++c32) {
+    for (int chunk = 0; chunk < D / S::kMergeDims; ++chunk) {
       float* mine = merge + warp * kHeadsOf * S::kMergePitch;
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < S::kMergeDims / 16; ++i)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const int dim = kE4M3 ? 16 * i + 2 * g4 + (x >> 1) : 16 * i + g4 + 8 * (x >> 1);
-            mine[(8 * n + 2 * t4 + (x & 1)) * S::kMergePitch + dim] = o[n][2 * c32 + i][x] * f[n][x & 1];
+            mine[(8 * n + 2 * t4 + (x & 1)) * S::kMergePitch + dim] = o[n][S::kMergeDims / 16 * chunk + i][x] * f[n][x & 1];
           }
-      workers_sync();
-      for (int i = tid; i < n_rows * 16; i += 32 * kWarps) {   // two dims of a head
-        const int rr = i >> 4, d2 = 2 * (i & 15), hl = (rr * group_inv) >> 16, row = rr - hl * group;
+      meet();
+      constexpr int kPairs = S::kMergeDims / 2;
+      for (int i = i0; i < my_rows * kPairs; i += step) {   // two dims of a head
+        const int rr = base_row + i / kPairs, d2 = 2 * (i % kPairs), hl = (rr * group_inv) >> 16, row = rr - hl * group;
         const float* src = merge + ((hl << strip_shift) * kHeadsOf + row) * S::kMergePitch + d2;
-        float2 part[kWarps];
+        float2 sum = *reinterpret_cast<const float2*>(src);
+        if (!alone) {
+          float2 part[kWarps - 1];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w)
-          part[w] = w < n_strips ? *reinterpret_cast<const float2*>(src + w * kHeadsOf * S::kMergePitch) : make_float2(0.f, 0.f);
-        float2 sum = part[0];
+          for (int w = 1; w < kWarps; ++w)
+            part[w - 1] = w < n_strips ? *reinterpret_cast<const float2*>(src + w * kHeadsOf * S::kMergePitch) : make_float2(0.f, 0.f);
 #pragma unroll
-        for (int w = 1; w < kWarps; ++w) {
-          sum.x += part[w].x;
-          sum.y += part[w].y;
+          for (int w = 1; w < kWarps; ++w) {
+            sum.x += part[w - 1].x;
+            sum.y += part[w - 1].y;
+          }
         }
         if (from_start && to_end) {
           const int h = (cur.block << heads_shift) * group + rr;
-          uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + cur.b * a.ld_out + static_cast<int64_t>(h) * D + 32 * c32 + d2);
+          uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + cur.b * a.ld_out + static_cast<int64_t>(h) * D + S::kMergeDims * chunk + d2);
           *out = kF16 ? pack_f16(sum.x, sum.y) : pack_bf16(sum.x, sum.y);
         } else {
-          *reinterpret_cast<float2*>(a.part_out + ((slot0 + (first ? 0 : 1)) * n_rows + rr) * D + 32 * c32 + d2) = sum;
+          *reinterpret_cast<float2*>(a.part_out + ((slot0 + (first ? 0 : 1)) * n_rows + rr) * D + S::kMergeDims * chunk + d2) = sum;
         }
       }
-      workers_sync();
+      meet();
     }
   };
 
@@ -562,9 +573,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 }
 
 // ---- parts of a sequence that several units worked on -------------------------------------------------
-// Weights 2^(lse_i - max) / sum over the parts, added in the parts' order.  A warp joins a row of few parts; the warps of a block share
-// 128 dims of a row of many (one long sequence is 148 parts: 300 KB of a latent row).
-constexpr int kJoinWarps = 8, kFewParts = 8, kManyDims = 128;
+// Weights 2^(lse_i - max) / sum over the parts, a fixed order of addition.  A warp joins a row of few parts, or 32 dims of a row of some;
+// the warps of a block share 32 dims of a row of many (a long sequence on its own is a part in every unit, and all SMs have to
+// fetch them together).
+constexpr int kJoinWarps = 8, kFewParts = 8, kSomeParts = 32, kManyDims = 32;
 template <typename T>
 __device__ __forceinline__ void store4(T* out, const float4& x) {
   uint2 w;
@@ -572,100 +584,130 @@ __device__ __forceinline__ void store4(T* out, const float4& x) {
   else w = make_uint2(pack_f16(x.x, x.y), pack_f16(x.z, x.w));
   *reinterpret_cast<uint2*>(out) = w;
 }
+// over lanes that differ in the bits from `from` on
+__device__ __forceinline__ float lanes_max(float x, int from) {
+  for (int o = from; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+  return x;
+}
+__device__ __forceinline__ float lanes_sum(float x, int from) {
+  for (int o = from; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+template <int V>
+struct IntC { static constexpr int value = V; };
+__device__ __forceinline__ void add(float4& x, float w, const float4& y) { x.x += w * y.x; x.y += w * y.y; x.z += w * y.z; x.w += w * y.w; }
+
 template <typename T>
 __global__ void __launch_bounds__(32 * kJoinWarps) paged_join_kernel(PagedAttnArgs a, int rows) {
   static_assert(paged::kJoinThreads == 32 * kJoinWarps, "threads of a block");
   __shared__ paged::JoinList list;
-  __shared__ float4 acc[kJoinWarps][32];
+  __shared__ float4 acc[kJoinWarps][8];
+  __shared__ float2 stats[kJoinWarps];   // {maximum, sum} of a warp's parts
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait();
   pdl_launch_dependents();
-  const int chunks = max(a.dv / kManyDims, 1), chunk_dims = min(a.dv, kManyDims);
-  auto rounds_of = [&](int n) { return n == 0 ? 0 : n <= kFewParts ? (rows + kJoinWarps - 1) / kJoinWarps : rows * chunks; };
+  const int chunks = a.dv / kManyDims;
+  auto rounds_of = [&](int n, int) {
+    return n == 0 ? 0 : n <= kFewParts ? (rows + kJoinWarps - 1) / kJoinWarps : n <= kSomeParts ? (rows * chunks + kJoinWarps - 1) / kJoinWarps : rows * chunks;
+  };
   int4 mine;
-  int begins;
-  const int total = paged::join_list(a, list, tid, &mine, &begins, rounds_of);
+  int begins, owners;
+  const int total = paged::join_list(a, list, tid, &mine, &begins, &owners, rounds_of);
   for (int it = blockIdx.x; it < total; it += gridDim.x) {   // block-uniform
-    paged::join_find(list, tid, it, mine, begins, rounds_of);
+    paged::join_find(list, tid, it, mine, begins, owners, rounds_of);
     const int4 own = list.own;
     const int n = own.x, round = list.round, unit = list.unit;
     auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (unit + i); };
-    // the weights of the parts of a row, a lane's being those of parts lane, lane + 32, ...
-    constexpr int kMine = (kMaxPagedUnits + 31) / 32;
-    auto weights = [&](int row, float (&w)[kMine], float* lse) {
-      float m = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < kMine; ++k) {
-        w[k] = 32 * k + lane < n ? __ldcg(a.part_lse + slot(32 * k + lane) * rows + row) : -INFINITY;
-        m = fmaxf(m, w[k]);
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      const float ref = m > -INFINITY ? m : 0.f;
-      float den = 0.f;
-#pragma unroll
-      for (int k = 0; k < kMine; ++k) {
-        w[k] = exp2f(w[k] - ref);
-        den += w[k];
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) den += __shfl_xor_sync(0xffffffffu, den, o);
-      const bool some = den > 0.f || den != den;
-      const float inv = some ? 1.f / den : 0.f;
-#pragma unroll
-      for (int k = 0; k < kMine; ++k) w[k] *= inv;
-      *lse = some ? (m + log2f(den)) / paged::kLog2e : -INFINITY;
-    };
-    float w[kMine], lse;
+    // (parts are asked for before their weights are known: one trip to L2)
     if (n <= kFewParts) {
       const int row = round * kJoinWarps + warp, d = 4 * lane;
-      if (row < rows) {   // whole warps
-        float4 y[kFewParts];   // (asked for before the weights are known: one trip to L2; a row has 64 or 128 dims)
+      if (row < rows) {   // whole warps; a row has 64 or 128 dims
+        float4 y[kFewParts];
 #pragma unroll
         for (int i = 0; i < kFewParts; ++i)
           if (i < n && d < a.dv) y[i] = __ldcg(reinterpret_cast<const float4*>(a.part_out + (slot(i) * rows + row) * a.dv + d));
-        weights(row, w, &lse);
+        const float lse = lane < n ? __ldcg(a.part_lse + slot(lane) * rows + row) : -INFINITY;
+        const float m = lanes_max(lse, 1);
+        float w = exp2f(lse - (m > -INFINITY ? m : 0.f));
+        const float den = lanes_sum(w, 1);
+        const bool some = den > 0.f || den != den;
+        w *= some ? 1.f / den : 0.f;
         const int h = own.z * rows + row;
-        if (lane == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(own.y) * a.H + h] = lse;
+        if (lane == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(own.y) * a.H + h] = some ? (m + log2f(den)) / paged::kLog2e : -INFINITY;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < kFewParts; ++i) {
-          const float wi = __shfl_sync(0xffffffffu, w[0], i);
-          if (i < n && d < a.dv) {
-            x.x += wi * y[i].x; x.y += wi * y[i].y; x.z += wi * y[i].z; x.w += wi * y[i].w;
-          }
+          const float wi = __shfl_sync(0xffffffffu, w, i);
+          if (i < n && d < a.dv) add(x, wi, y[i]);
         }
         if (d < a.dv) store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d, x);
       }
     } else {
-      const int row = round / chunks, d0 = (round - row * chunks) * chunk_dims;
-      const int h = own.z * rows + row;
-      weights(row, w, &lse);
-      if (tid == 0 && d0 == 0 && a.lse != nullptr) a.lse[static_cast<int64_t>(own.y) * a.H + h] = lse;
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      const bool on = 4 * lane < chunk_dims;
-      const float* src = a.part_out + static_cast<int64_t>(row) * a.dv + d0 + (on ? 4 * lane : 0);
+      // Eight lanes a part, four parts a warp at a time: parts first + lane / 8, `apart` further, ...
+      const bool own_warp = n <= kSomeParts;
+      const int piece = own_warp ? round * kJoinWarps + warp : round;
+      const int row = piece / chunks, d0 = (piece - row * chunks) * kManyDims, h = own.z * rows + row, c = lane & 7;
+      auto gather = [&](auto mine_c, int first, int apart, float4* sum, float* top, float* den) {   // of the warp's parts, relative to their maximum
+        constexpr int kMine = decltype(mine_c)::value;
+        const float* src = a.part_out + static_cast<int64_t>(row) * a.dv + d0 + 4 * c;
+        float4 y[kMine];
+        float w[kMine], m = -INFINITY, all = 0.f;
 #pragma unroll
-      for (int k = 0; k < kMine; ++k) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {   // parts 32 k + 8 j + warp
-          const int i = 32 * k + 8 * j + warp;
-          const float wi = __shfl_sync(0xffffffffu, w[k], 8 * j + warp);
+        for (int k = 0; k < kMine; ++k) {
+          const int i = apart * k + first + (lane >> 3);
+          w[k] = -INFINITY;
+          y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
           if (i < n) {
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(src + slot(i) * rows * a.dv));
-            x.x += wi * y.x; x.y += wi * y.y; x.z += wi * y.z; x.w += wi * y.w;
+            w[k] = __ldcg(a.part_lse + slot(i) * rows + row);
+            y[k] = __ldcg(reinterpret_cast<const float4*>(src + slot(i) * rows * a.dv));
           }
+          m = fmaxf(m, w[k]);
         }
-      }
-      acc[warp][lane] = x;
-      __syncthreads();
-      if (warp == 0) {
+        m = lanes_max(m, 8);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int i = 1; i < kJoinWarps; ++i) {
-          const float4 y = acc[i][lane];
-          x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+        for (int k = 0; k < kMine; ++k) {
+          w[k] = exp2f(w[k] - (m > -INFINITY ? m : 0.f));
+          all += w[k];
+          add(x, w[k], y[k]);
         }
-        if (on) store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d0 + 4 * lane, x);
+        *top = m;
+        *den = lanes_sum(all, 8);
+        *sum = make_float4(lanes_sum(x.x, 8), lanes_sum(x.y, 8), lanes_sum(x.z, 8), lanes_sum(x.w, 8));
+      };
+      auto write = [&](const float4& x, float top, float den) {   // the sum, undivided, by eight lanes
+        const bool some = den > 0.f || den != den;
+        const float inv = some ? 1.f / den : 0.f;
+        if (lane < 8)
+          store4(static_cast<T*>(a.out) + own.y * a.ld_out + static_cast<int64_t>(h) * a.dv + d0 + 4 * lane,
+                 make_float4(x.x * inv, x.y * inv, x.z * inv, x.w * inv));
+        if (lane == 0 && d0 == 0 && a.lse != nullptr)
+          a.lse[static_cast<int64_t>(own.y) * a.H + h] = some ? (top + log2f(den)) / paged::kLog2e : -INFINITY;
+      };
+      float4 x;
+      float m, den;
+      if (own_warp) {
+        if (row < rows) {   // whole warps
+          gather(IntC<kSomeParts / 4>{}, 0, 4, &x, &m, &den);
+          write(x, m, den);
+        }
+      } else {
+        gather(IntC<(kMaxPagedUnits + 4 * kJoinWarps - 1) / (4 * kJoinWarps)>{}, 4 * warp, 4 * kJoinWarps, &x, &m, &den);
+        if (lane < 8) acc[warp][lane] = x;
+        if (lane == 0) stats[warp] = make_float2(m, den);
+        __syncthreads();
+        if (warp == 0) {
+          const float2 s = stats[lane & 7];
+          float top = s.x;
+          for (int o = 1; o < 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          const float f = exp2f(s.x - (top > -INFINITY ? top : 0.f));
+          float all = f * s.y;
+          for (int o = 1; o < 8; o <<= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+          x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int i = 0; i < kJoinWarps; ++i) add(x, __shfl_sync(0xffffffffu, f, i), acc[i][c]);
+          write(x, top, all);
+        }
       }
     }
   }

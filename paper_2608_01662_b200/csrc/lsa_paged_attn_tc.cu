@@ -523,9 +523,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
 
 // ---- parts of a sequence that several units worked on
 // Weights 2^(lse_i - max) / sum over the parts, a fixed order of addition.  A part is [dim][64 heads], so a thread has one head.  A
-// round of a block: few parts: 64 dims, 16 of them per thread; many (one long sequence is 148 parts of 128 KB, which all SMs have to
-// fetch together): two dims, four threads sharing the parts of a head.
-constexpr int kJoinThreads = paged::kJoinThreads, kFewParts = 8, kFewDims = 64, kManyDims = 2, kWays = 4;
+// round of a block is 64 dims where a sequence has a few parts, 16 with up to 16 parts of many sequences, and else (one long sequence is
+// 148 parts of 128 KB, which all SMs have to fetch together) two, four threads sharing a head's parts.  (16 sequences of 777 tokens, 7 parts
+// each: 22.6 us with two dims a round, 20.3 with 16; one, 13 parts: 13.1 and 15.9.)
+constexpr int kJoinThreads = paged::kJoinThreads, kWays = 4;
+constexpr int kFewParts = 4, kFewDims = 64, kSomeParts = 16, kSomeDims = 16, kSomeOwners = 8, kManyDims = 2;
+template <int V>
+struct IntC { static constexpr int value = V; };
+
 template <bool kF16>
 __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAttnArgs a) {
   __shared__ paged::JoinList list;
@@ -534,12 +539,13 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
   const int tid = threadIdx.x, head = tid & 63, way = tid >> 6;
   pdl_wait();
   pdl_launch_dependents();
-  auto rounds_of = [](int n) { return n == 0 ? 0 : n <= kFewParts ? kDV / kFewDims : kDV / kManyDims; };
+  auto dims_of = [](int n, int owners) { return n <= kFewParts ? kFewDims : n <= kSomeParts && owners >= kSomeOwners ? kSomeDims : kManyDims; };
+  auto rounds_of = [&](int n, int owners) { return n == 0 ? 0 : kDV / dims_of(n, owners); };
   int4 mine;
-  int begins;
-  const int total = paged::join_list(a, list, tid, &mine, &begins, rounds_of);
+  int begins, owners;
+  const int total = paged::join_list(a, list, tid, &mine, &begins, &owners, rounds_of);
   for (int it = blockIdx.x; it < total; it += gridDim.x) {   // block-uniform
-    paged::join_find(list, tid, it, mine, begins, rounds_of);
+    paged::join_find(list, tid, it, mine, begins, owners, rounds_of);
     const int4 own = list.own;
     const int n = own.x, round = list.round, unit = list.unit;
     auto slot = [&](int i) -> int64_t { return i == 0 ? own.w : 2 * (unit + i); };
@@ -550,26 +556,26 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
         a.lse[static_cast<int64_t>(own.y) * a.H + head] = some ? (m + log2f(den)) / paged::kLog2e : -INFINITY;
       return some ? 1.f / den : 0.f;
     };
-    if (n <= kFewParts) {
-      float w[kFewParts], m = -INFINITY, den = 0.f;
+    auto several = [&](auto parts_c, auto dims_c) {   // up to so many parts, so many dims
+      constexpr int kParts = decltype(parts_c)::value, kDims = decltype(dims_c)::value, kMine = kDims / kWays;
+      float w[kParts], m = -INFINITY, den = 0.f;
 #pragma unroll
-      for (int i = 0; i < kFewParts; ++i) {
+      for (int i = 0; i < kParts; ++i) {
         w[i] = i < n ? __ldcg(a.part_lse + slot(i) * kHeads + head) : -INFINITY;
         m = fmaxf(m, w[i]);
       }
       const float ref = m > -INFINITY ? m : 0.f;
 #pragma unroll
-      for (int i = 0; i < kFewParts; ++i) {
+      for (int i = 0; i < kParts; ++i) {
         w[i] = exp2f(w[i] - ref);
         den += w[i];
       }
       const float inv = finish(m, den);
-      constexpr int kMine = kFewDims / kWays;
       float x[kMine] = {};
 #pragma unroll
-      for (int i = 0; i < kFewParts; ++i) {
+      for (int i = 0; i < kParts; ++i) {
         if (i < n) {
-          const float* src = a.part_out + (slot(i) * kDV + round * kFewDims + way * kMine) * kHeads + head;
+          const float* src = a.part_out + (slot(i) * kDV + round * kDims + way * kMine) * kHeads + head;
           const float wi = w[i] * inv;
 #pragma unroll
           for (int j = 0; j < kMine; ++j) x[j] += wi * __ldcg(src + j * kHeads);
@@ -578,10 +584,16 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
 #pragma unroll
       for (int j = 0; j < kMine; j += 2) tile[head][(way * kMine + j) / 2] = pack2<kF16>(x[j], x[j + 1]);
       __syncthreads();
-      for (int i = tid; i < a.H * (kFewDims / 2); i += kJoinThreads) {
-        const int row = i / (kFewDims / 2), d = i % (kFewDims / 2);
-        *reinterpret_cast<uint32_t*>(out + row * kDV + round * kFewDims + 2 * d) = tile[row][d];
+      for (int i = tid; i < a.H * (kDims / 2); i += kJoinThreads) {
+        const int row = i / (kDims / 2), d = i % (kDims / 2);
+        *reinterpret_cast<uint32_t*>(out + row * kDV + round * kDims + 2 * d) = tile[row][d];
       }
+    };
+    const int dims = dims_of(n, owners);
+    if (dims == kFewDims) {
+      several(IntC<kFewParts>{}, IntC<kFewDims>{});
+    } else if (dims == kSomeDims) {
+      several(IntC<kSomeParts>{}, IntC<kSomeDims>{});
     } else {
       float m = -INFINITY, den = 0.f;
       const float* lse = a.part_lse + head;
