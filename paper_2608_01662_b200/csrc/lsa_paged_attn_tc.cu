@@ -7,14 +7,14 @@
 //
 //   warp 8      copies: a tile lies inside one cache page, so each half of it is one TMA box (nine column blocks of 32 rows x 128
 //               bytes, 128B-swizzled), into a ring of six such slots.  Every slot is 36.9 KB.
-//   warp 9      S = Q K^T, M64 N32 K16, Q in tensor memory (its last 64 dims in shared memory), as two accumulation chains
+//   warps 9, 10 S = Q K^T, a half of the tile each, M64 N32 K16, Q in tensor memory (its last 64 dims in shared memory), as two accumulation chains
 //               in the two halves of the lanes (an M = 64 accumulator uses 16 lanes of each 32); two S buffers.
 //   warps 0-7   softmax, four warps for each half of a tile's keys: the two partial sums are added, P = 2^(score - max) with the running
 //               maximum as it is, fp32 row sums, P in 16 bits into the slot's last column block, which only Q K^T reads; one vote
 //               says whether the maximum was good enough for every row (O is rescaled, and P worked out again, only when a row
 //               grows by more than 2^8).  At a sequence's end they fetch the next Q and write O.  Rows of a tile that nobody
 //               sees are zeroed there before they become values: 0 x NaN is NaN.
-//   warp 10     O += P V, tcgen05.mma.ws M64 N256 K16; V is the tile read MN-major, so a row is fetched once.
+//   warp 11     O += P V, tcgen05.mma.ws M64 N256 K16; V is the tile read MN-major, so a row is fetched once.
 //
 // Tensor memory columns:   0-255  O: value dims 0-255 in columns 0-127, 256-511 in 128-255; lanes 0-63 hold the first 128
 //                                 dims of each, lanes 64-127 the second, lane l (mod 64) = head l
@@ -37,7 +37,7 @@ constexpr int kHalfKeys = kTileKeys / 2, kGroups = kHalfKeys / 8;   // keys of a
 constexpr int kAtomBytes = kHalfKeys * 128;
 constexpr int kSlotBytes = kAtoms * kAtomBytes;
 constexpr int kRing = 3;                                            // tiles, two slots each
-constexpr int kSoftmaxWarps = 8, kCopyWarp = 8, kQkWarp = 9, kPvWarp = 10, kThreads = 352;
+constexpr int kSoftmaxWarps = 8, kCopyWarp = 8, kQkWarp = 9, kPvWarp = 11, kThreads = 384;
 constexpr int kSoftmaxThreads = 32 * kSoftmaxWarps;
 constexpr uint32_t kTmemCols = 512, kColQ = 256, kColS = 384, kSBuf = 64;
 constexpr float kRescaleGap = 8.f;   // O is rescaled only when a row's maximum grows by more than 2^8
@@ -168,13 +168,14 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
     // every copy has landed before the block ends, also if somebody gave up on a wait
     for (int i = max(issued - 2 * kRing, 0); i < issued; ++i)
       (void)tc::mbar_wait(smem_u32(&sm.k_full[i % (2 * kRing)]), static_cast<uint32_t>(i / (2 * kRing)) & 1u, nullptr);
-  } else if (warp == kQkWarp) {
+  } else if (warp == kQkWarp || warp == kQkWarp + 1) {
     // ================= S = Q K^T =================
     if (tc::elect_one()) {
       const uint64_t dk0 = tc::smem_desc_sw128(smem_u32(sm.k), 16, 1024);
       const uint64_t dqr = tc::smem_desc_sw128(smem_u32(sm.q_rope), 16, 1024);
       constexpr uint32_t idesc = idesc_16<kF16>(kHeads, kHalfKeys, 0, 0);
       constexpr uint32_t kLane16 = 16u << 16;
+      const int h = warp - kQkWarp;   // the half of the tiles
       bool fresh = true, ok = true;
       uint32_t piece = 0, use = 0;
       int pair = 0;
@@ -187,30 +188,26 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       for (int g = 0; g < entries && ok; ++g) {
         if (fresh) {
           if (!tc::mbar_wait(smem_u32(&sm.q_ready), piece++ & 1u, a.status)) break;
-          tc::mbar_arrive(smem_u32(&sm.k_empty[2 * pair]));   // Q has left its slots
-          tc::mbar_arrive(smem_u32(&sm.k_empty[2 * pair + 1]));
+          tc::mbar_arrive(smem_u32(&sm.k_empty[2 * pair + h]));   // Q has left its slots
           next();
         }
         const int buf = g & 1;
-#pragma unroll 1
-        for (int h = 0; h < 2; ++h) {
-          ok = tc::mbar_wait(smem_u32(&sm.k_full[2 * pair + h]), use, a.status) &&
-               tc::mbar_wait(smem_u32(&sm.s_free[2 * buf + h]), (static_cast<uint32_t>(g >> 1) & 1u) ^ 1u, a.status);
-          if (!ok) break;
-          tc::fence_after_sync();
-          const uint64_t dk = tc::desc_advance(dk0, (2 * pair + h) * kSlotBytes);
+        ok = tc::mbar_wait(smem_u32(&sm.k_full[2 * pair + h]), use, a.status) &&
+             tc::mbar_wait(smem_u32(&sm.s_free[2 * buf + h]), (static_cast<uint32_t>(g >> 1) & 1u) ^ 1u, a.status);
+        if (!ok) break;
+        tc::fence_after_sync();
+        const uint64_t dk = tc::desc_advance(dk0, (2 * pair + h) * kSlotBytes);
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint32_t q_src = tmem_base + x * kLane16 + kColQ, s_dst = tmem_base + x * kLane16 + kColS + buf * kSBuf + kHalfKeys * h;
+        for (int x = 0; x < 2; ++x) {
+          const uint32_t q_src = tmem_base + x * kLane16 + kColQ, s_dst = tmem_base + x * kLane16 + kColS + buf * kSBuf + kHalfKeys * h;
 #pragma unroll
-            for (int s = 0; s < 16; ++s)   // dims 256 x + 16 s .. + 15
-              tc::umma_ts(s_dst, q_src + 8 * s, tc::desc_advance(dk, (4 * x + (s >> 2)) * kAtomBytes + (s & 3) * 32), idesc, s != 0);
+          for (int s = 0; s < 16; ++s)   // dims 256 x + 16 s .. + 15
+            tc::umma_ts(s_dst, q_src + 8 * s, tc::desc_advance(dk, (4 * x + (s >> 2)) * kAtomBytes + (s & 3) * 32), idesc, s != 0);
 #pragma unroll
-            for (int s = 0; s < 2; ++s)    // dims 512 + 32 x + 16 s .. + 15
-              tc::umma_ss(s_dst, tc::desc_advance(dqr, (2 * x + s) * 32), tc::desc_advance(dk, 8 * kAtomBytes + (2 * x + s) * 32), idesc, 1);
-          }
-          tc::umma_commit(smem_u32(&sm.s_full[2 * buf + h]));
+          for (int s = 0; s < 2; ++s)    // dims 512 + 32 x + 16 s .. + 15
+            tc::umma_ss(s_dst, tc::desc_advance(dqr, (2 * x + s) * 32), tc::desc_advance(dk, 8 * kAtomBytes + (2 * x + s) * 32), idesc, 1);
         }
+        tc::umma_commit(smem_u32(&sm.s_full[2 * buf + h]));
         next();
         fresh = paged::advance(a, cur, kShift, 1);
       }
