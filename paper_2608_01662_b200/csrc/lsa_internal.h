@@ -257,7 +257,7 @@ struct PagedAttnArgs {
   const int32_t* ctx_len;
   void* out;
   float* lse;
-  float* part_out;            // fp32 [2 * units][rows of a unit][dv] (latent: [dv][64 heads]), normalised
+  float* part_out;            // fp32 [2 * units][rows of a unit][dv] (latent: [dv / 4][64 heads][4]), normalised
   float* part_lse;            // fp32 [2 * units][rows of a unit], log2
   int4* parts;                // [units]: what there is to join
   int* status;

@@ -478,7 +478,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       const float inv = sm.factor[head_o];
       const int dim0 = 256 * half + 128 * half_o;
       uint8_t* stage = &sm.k[2 * this_pair][0][0];   // whole results: rows of 1024 bytes, 16-byte units XORed with the row, over two slots
-      float* part = a.part_out + ((2 * static_cast<int64_t>(blockIdx.x) + (first ? 0 : 1)) * kDV + dim0) * kHeads + head_o;
+      float* part = a.part_out + ((2 * static_cast<int64_t>(blockIdx.x) + (first ? 0 : 1)) * kDV + dim0) * kHeads + 4 * head_o;
 #pragma unroll 1
       for (int c = 0; c < 128; c += 32) {
         uint32_t o[32];
@@ -492,9 +492,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
             for (int i = 0; i < 4; ++i) w[i] = pack2<kF16>(__uint_as_float(o[8 * j + 2 * i]) * inv, __uint_as_float(o[8 * j + 2 * i + 1]) * inv);
             *reinterpret_cast<uint4*>(stage + head_o * 1024 + ((((dim0 + c) / 8 + j) ^ (head_o & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-        } else {   // a part: the lanes' heads lie side by side (a row of its own per lane took 10 thousand cycles to store)
+        } else {   // a part: four dims of each head, the lanes' heads side by side (a row of its own per lane took 10 thousand cycles to store)
 #pragma unroll
-          for (int j = 0; j < 32; ++j) part[(c + j) * kHeads] = __uint_as_float(o[j]) * inv;
+          for (int j = 0; j < 8; ++j)
+            *reinterpret_cast<float4*>(part + (c + 4 * j) * kHeads) =
+                make_float4(__uint_as_float(o[4 * j]) * inv, __uint_as_float(o[4 * j + 1]) * inv, __uint_as_float(o[4 * j + 2]) * inv,
+                            __uint_as_float(o[4 * j + 3]) * inv);
         }
       }
       tc::fence_before_sync();   // O has been read: the next sequence's P V may begin once its first P is there
@@ -519,20 +522,24 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
 }
 
 // ---- parts of a sequence that several units worked on
-// Weights 2^(lse_i - max) / sum over the parts, a fixed order of addition.  A part is [dim][64 heads], so a thread has one head.  A
-// round of a block is 64 dims where a sequence has a few parts, 16 with up to 16 parts of many sequences, and else (one long sequence is
-// 148 parts of 128 KB, which all SMs have to fetch together) two, four threads sharing a head's parts.  (16 sequences of 777 tokens, 7 parts
-// each: 22.6 us with two dims a round, 20.3 with 16; one, 13 parts: 13.1 and 15.9.)
+// Weights 2^(lse_i - max) / sum over the parts, a fixed order of addition.  A part is [dim / 4][64 heads][4 dims], so a thread has one
+// head and a warp's loads are 512 bytes.  A round of a block is 64 dims where a sequence has a few parts, 16 with up to eight parts of
+// many sequences, and else (one long sequence is 148 parts of 128 KB, which all SMs have to fetch together) four, four threads
+// sharing a head's parts.  (16 sequences of 777 tokens, 7 parts each: 23.8 us by fours, 19.2 so; by 16 for up to 16 parts 23.2,
+// the loop is then as long for all.)  Two blocks an SM: at 64 registers, four of them, the loads are no longer on their way together
+// (one sequence of 8000 tokens 15.3 us, 20.6).
 constexpr int kJoinThreads = paged::kJoinThreads, kWays = 4;
-constexpr int kFewParts = 4, kFewDims = 64, kSomeParts = 16, kSomeDims = 16, kSomeOwners = 8, kManyDims = 2;
+constexpr int kFewParts = 4, kFewDims = 64, kSomeParts = 8, kSomeDims = 16, kSomeOwners = 8, kManyDims = 4, kManyAtOnce = 10;
 template <int V>
 struct IntC { static constexpr int value = V; };
+__device__ __forceinline__ void add(float4& x, float w, const float4& y) { x.x += w * y.x; x.y += w * y.y; x.z += w * y.z; x.w += w * y.w; }
 
 template <bool kF16>
-__global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, 2) paged_latent_join_kernel(PagedAttnArgs a) {
   __shared__ paged::JoinList list;
   __shared__ uint32_t tile[kHeads][kFewDims / 2 + 1];
-  __shared__ float red[kWays][kHeads][2];
+  __shared__ float4 red[kWays][kHeads];
+  __shared__ float2 stats[kWays][kHeads];   // {maximum, sum} of a thread's parts
   const int tid = threadIdx.x, head = tid & 63, way = tid >> 6;
   pdl_wait();
   pdl_launch_dependents();
@@ -568,18 +575,21 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
         den += w[i];
       }
       const float inv = finish(m, den);
-      float x[kMine] = {};
+      float4 x[kMine / 4] = {};
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
         if (i < n) {
-          const float* src = a.part_out + (slot(i) * kDV + round * kDims + way * kMine) * kHeads + head;
+          const float* src = a.part_out + (slot(i) * kDV + round * kDims + way * kMine) * kHeads + 4 * head;
           const float wi = w[i] * inv;
 #pragma unroll
-          for (int j = 0; j < kMine; ++j) x[j] += wi * __ldcg(src + j * kHeads);
+          for (int j = 0; j < kMine / 4; ++j) add(x[j], wi, __ldcg(reinterpret_cast<const float4*>(src + 4 * j * kHeads)));
         }
       }
 #pragma unroll
-      for (int j = 0; j < kMine; j += 2) tile[head][(way * kMine + j) / 2] = pack2<kF16>(x[j], x[j + 1]);
+      for (int j = 0; j < kMine / 4; ++j) {
+        tile[head][way * kMine / 2 + 2 * j] = pack2<kF16>(x[j].x, x[j].y);
+        tile[head][way * kMine / 2 + 2 * j + 1] = pack2<kF16>(x[j].z, x[j].w);
+      }
       __syncthreads();
       for (int i = tid; i < a.H * (kDims / 2); i += kJoinThreads) {
         const int row = i / (kDims / 2), d = i % (kDims / 2);
@@ -592,39 +602,56 @@ __global__ void __launch_bounds__(kJoinThreads) paged_latent_join_kernel(PagedAt
     } else if (dims == kSomeDims) {
       several(IntC<kSomeParts>{}, IntC<kSomeDims>{});
     } else {
+      // the thread's parts, kManyAtOnce on their way at a time, relative to their maximum so far
       float m = -INFINITY, den = 0.f;
-      const float* lse = a.part_lse + head;
-      for (int i = way; i < n; i += kWays) m = fmaxf(m, __ldcg(lse + slot(i) * kHeads));
-      red[way][head][0] = m;
-      __syncthreads();
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+      const float* src = a.part_out + static_cast<int64_t>(round) * kManyDims * kHeads + 4 * head;
+      for (int i0 = way; i0 < n; i0 += kManyAtOnce * kWays) {
+        float4 y[kManyAtOnce];
+        float w[kManyAtOnce], top = m;
 #pragma unroll
-      for (int i = 0; i < kWays; ++i) m = fmaxf(m, red[i][head][0]);
-      const float ref = m > -INFINITY ? m : 0.f;
-      float x[2] = {0.f, 0.f};
-      const float* src = a.part_out + static_cast<int64_t>(round) * kManyDims * kHeads + head;
-#pragma unroll 8
-      for (int i = way; i < n; i += kWays) {
-        const float w = exp2f(__ldcg(lse + slot(i) * kHeads) - ref);
-        const float* p = src + slot(i) * kDV * kHeads;
-        const float x0 = __ldcg(p), x1 = __ldcg(p + kHeads);
-        den += w;
-        x[0] += w * x0;
-        x[1] += w * x1;
+        for (int k = 0; k < kManyAtOnce; ++k) {
+          const int i = i0 + k * kWays;
+          w[k] = -INFINITY;
+          y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i < n) {
+            w[k] = __ldcg(a.part_lse + slot(i) * kHeads + head);
+            y[k] = __ldcg(reinterpret_cast<const float4*>(src + slot(i) * kDV * kHeads));
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kManyAtOnce; ++k) top = fmaxf(top, w[k]);
+        const float ref = top > -INFINITY ? top : 0.f, old = exp2f(m - ref);
+        m = top;
+        den *= old;
+        x = make_float4(x.x * old, x.y * old, x.z * old, x.w * old);
+#pragma unroll
+        for (int k = 0; k < kManyAtOnce; ++k) {
+          const float e = exp2f(w[k] - ref);
+          den += e;
+          add(x, e, y[k]);
+        }
       }
-      __syncthreads();   // (the maxima have been read)
-      red[way][head][0] = den;
-      red[way][head][1] = x[0];
-      reinterpret_cast<float*>(tile)[tid] = x[1];
+      red[way][head] = x;
+      stats[way][head] = make_float2(m, den);
       __syncthreads();
       if (way == 0) {
+        float top = m;
 #pragma unroll
-        for (int i = 1; i < kWays; ++i) {
-          den += red[i][head][0];
-          x[0] += red[i][head][1];
-          x[1] += reinterpret_cast<const float*>(tile)[64 * i + head];
+        for (int i = 1; i < kWays; ++i) top = fmaxf(top, stats[i][head].x);
+        const float ref = top > -INFINITY ? top : 0.f;
+        x = make_float4(0.f, 0.f, 0.f, 0.f);
+        den = 0.f;
+#pragma unroll
+        for (int i = 0; i < kWays; ++i) {
+          const float2 s = stats[i][head];
+          const float f = exp2f(s.x - ref);
+          den += f * s.y;
+          add(x, f, red[i][head]);
         }
-        const float inv = finish(m, den);
-        if (head < a.H) *reinterpret_cast<uint32_t*>(out + head * kDV + round * kManyDims) = pack2<kF16>(x[0] * inv, x[1] * inv);
+        const float inv = finish(top, den);
+        if (head < a.H)
+          *reinterpret_cast<uint2*>(out + head * kDV + round * kManyDims) = make_uint2(pack2<kF16>(x.x * inv, x.y * inv), pack2<kF16>(x.z * inv, x.w * inv));
       }
     }
   }
@@ -649,7 +676,7 @@ cudaError_t launch_paged_attn_tc(const PagedAttnArgs& a, cudaStream_t st, int64_
   if (e != cudaSuccess) return e;
   ++*n_launch;
   auto join = a.fp16 ? paged_latent_join_kernel<true> : paged_latent_join_kernel<false>;
-  e = launch_pdl(join, dim3(4 * a.units), dim3(kJoinThreads), 0, st, a);
+  e = launch_pdl(join, dim3(2 * a.units), dim3(kJoinThreads), 0, st, a);
   if (e == cudaSuccess) e = cudaGetLastError();
   if (e == cudaSuccess) ++*n_launch;
   return e;

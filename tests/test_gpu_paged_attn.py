@@ -60,6 +60,20 @@ def test_long_sequences_are_split_and_joined(cuda_device, lengths, shape, dtype,
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])   # the same call gives the same bits
 
 
+@pytest.mark.parametrize("shape", [(32, 8, 128, 128), (16, 1, 128, 128), (12, 4, 64, 64), (9, 3, 64, 64)])
+@pytest.mark.parametrize("lengths", [[130], [300] * 3, [500, 500], [700] * 9, [1500, 40, 1500], [2500, 6000]])
+def test_joins_of_few_some_and_many_parts(cuda_device, shape, lengths):
+    """Sequences in 2 to 100 parts, alone and several of them."""
+    c = pu.Cache(lengths, shape, 16, "bf16", False, cuda_device, seed=sum(lengths) + shape[0], poison=True)
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse)
+    out2 = torch.empty_like(out)
+    ctx.paged_attn(c.q, c.k, c.v, c.page_table, c.ctx_len, out2)
+    torch.cuda.synchronize()
+    assert torch.equal(out, out2)
+
+
 def test_large_batches(cuda_device):
     rng = np.random.default_rng(5)
     lengths = [int(x) for x in rng.integers(0, 90, 700)]

@@ -52,6 +52,20 @@ def test_long_sequences_are_split_and_joined(cuda_device, lengths):
     assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
 
 
+@pytest.mark.parametrize("heads", [64, 7])
+@pytest.mark.parametrize("lengths", [[130], [250] * 3, [400] * 12, [777] * 10, [1300] * 9, [2000, 70, 900]])
+def test_joins_of_few_some_and_many_parts(cuda_device, heads, lengths):
+    """Sequences in 2 to 32 parts, alone and several of them."""
+    c = pu.Cache(lengths, (heads, 1, 576, 512), 64, "bf16", False, cuda_device, seed=sum(lengths) + heads, poison=True)
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse)
+    out2 = torch.empty_like(out)
+    ctx.paged_attn(c.q, c.k, None, c.page_table, c.ctx_len, out2)
+    torch.cuda.synchronize()
+    assert torch.equal(out, out2)
+
+
 def test_many_short_sequences(cuda_device):
     rng = np.random.default_rng(5)
     lengths = [int(x) for x in rng.integers(0, 150, 500)]
