@@ -81,7 +81,7 @@ __device__ __forceinline__ void workers_sync() { asm volatile("bar.sync 1, %0;" 
 // heads_shift: log2 of the KV heads that a block works on at the same time (8, 4, 2 or 1, a divisor of G).
 template <typename T, int D, bool kE4M3, int kTiles>
 __global__ void __launch_bounds__(kThreads, 1)
-paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, PagedAttnArgs a, int heads_shift) {
+paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, PagedAttnArgs p, int heads_shift) {
   using S = Shape<D, kE4M3, kTiles>;
   constexpr bool kF16 = !__is_same(T, __nv_bfloat16);
   constexpr bool kQkF16 = kF16 || kE4M3, kPvF16 = kF16 && !kE4M3;
@@ -95,8 +95,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int strip_shift = 3 - heads_shift, n_strips = 1 << strip_shift;
   const int shift = S::kRowShift + strip_shift;     // keys of a tile
-  const int blocks = a.G >> heads_shift;
-  const int box_shift = min(shift, a.page_shift);   // keys of a box
+  const int blocks = p.G >> heads_shift;
+  const int box_shift = min(shift, p.page_shift);   // keys of a box
 
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
@@ -109,15 +109,15 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   }
   pdl_wait();
   pdl_launch_dependents();
-  const bool raised = tc::status_raised(a.status);
-  Cursor cur = paged::first_entry(a, blockIdx.x, shift, blocks, lane);
+  const bool raised = tc::status_raised(p.status);
+  Cursor cur = paged::first_entry(p, blockIdx.x, shift, blocks, lane);
   const bool dead = __syncthreads_or(raised) != 0;   // the same in all threads
   if (dead) return;
 
   if (warp == kWarps) {
     // ================= copies =================
-    const int page_mask = (1 << a.page_shift) - 1;
-    const int beyond = static_cast<int>(static_cast<int64_t>(max(a.n_pages, 1)) << a.page_shift);   // the first row past the pool: rows of zeros
+    const int page_mask = (1 << p.page_shift) - 1;
+    const int beyond = static_cast<int>(static_cast<int64_t>(max(p.n_pages, 1)) << p.page_shift);   // the first row past the pool: rows of zeros
     const int box_bytes = (S::kBytes >> shift) << box_shift;   // (a tile's bytes over its keys, times a box's)
     const int n_boxes = 1 << (shift - box_shift);
     // a lane's box of the tile at the cursor: its cache row; past the pool if its page is not one, -1 if nobody sees its keys
@@ -125,12 +125,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
       if (cur.left <= 0 || lane >= n_boxes) return -1;
       const int s0 = cur.st.first_key(cur.tile, shift) + (lane << box_shift);
       if (!cur.st.any_seen(s0, 1 << box_shift)) return -1;
-      const int p = a.page_table[cur.b * a.pt_stride + (s0 >> a.page_shift)];
-      if (p < 0 || p >= a.n_pages) {
-        paged::report_index(a.notice);
+      const int page = p.page_table[cur.b * p.pt_stride + (s0 >> p.page_shift)];
+      if (page < 0 || page >= p.n_pages) {
+        paged::report_index(p.notice);
         return beyond;
       }
-      return (p << a.page_shift) + (s0 & page_mask);
+      return (page << p.page_shift) + (s0 & page_mask);
     };
     int row = row_of(), slot = 0;
     uint32_t use = 0;
@@ -139,12 +139,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     bool alive = true;
     for (int g = 0; g < entries && alive; ++g) {
       const int this_row = row, head0 = cur.block << heads_shift;
-      paged::advance(a, cur, shift, blocks);
+      paged::advance(p, cur, shift, blocks);
       row = row_of();   // (its page number is on its way while this tile waits for its slots)
       const int n_here = __popc(__ballot_sync(0xffffffffu, this_row >= 0));
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
-        alive = alive && __all_sync(0xffffffffu, tc::mbar_wait(empty + 8 * slot, use ^ 1u, a.status));
+        alive = alive && __all_sync(0xffffffffu, tc::mbar_wait(empty + 8 * slot, use ^ 1u, p.status));
         if (!alive) break;
         const uint32_t bar = full + 8 * slot;
         if (lane == 0) tc::mbar_expect_tx(bar, static_cast<uint32_t>(n_here * box_bytes));
@@ -152,14 +152,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (this_row >= 0)
           tc::tma_load_3d(smem_u32(ring) + slot * S::kBytes + lane * box_bytes, kv == 0 ? &k_map : &v_map, 0, this_row, head0 * S::kBlocks, bar);
         if constexpr (kE4M3) {
-          const float* src = kv == 0 ? a.k_scale : a.v_scale;
+          const float* src = kv == 0 ? p.k_scale : p.v_scale;
           const uint32_t dst = smem_u32(scales) + slot * S::kScales;
           for (int j = 0; j < n_boxes; ++j) {   // rows of 4, 8, 16 or 32 bytes, a lane each
             const int r0 = __shfl_sync(0xffffffffu, this_row, j);
             if (r0 < 0) continue;
             for (int i = lane; i < 1 << box_shift; i += 32) {
               const int r = (j << box_shift) + i;
-              const float* s = src + (r0 < beyond ? static_cast<int64_t>(r0 + i) * a.G + head0 : 0);
+              const float* s = src + (r0 < beyond ? static_cast<int64_t>(r0 + i) * p.G + head0 : 0);
               const bool there = r0 < beyond;
               if (heads_shift == 0) cp_async_ca<4>(dst + r * 4, s, there ? 4 : 0);
               else if (heads_shift == 1) cp_async_ca<8>(dst + r * 8, s, there ? 8 : 0);
@@ -185,8 +185,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   // ================= strips =================
   const int g4 = lane >> 2, t4 = lane & 3;
   const int head_l = warp >> strip_shift, strip = warp & (n_strips - 1);
-  const int group = a.H / a.G;
-  if (cur.left == 0 && tid == 0) a.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
+  const int group = p.H / p.G;
+  if (cur.left == 0 && tid == 0) p.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
 
   // Where the strip lies in a slot: boxes of [block of columns][key][block bytes], 16-byte units XORed as TMA does it, which also keeps the
   // eight rows that an ldmatrix phase reads in different banks.  A strip of 32 tokens in pages of 16 lies in two boxes.
@@ -216,12 +216,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   float zs[kTiles][2], m_used[kTiles][2], l_run[kTiles][2];
   auto begin = [&]() {
     const int head0 = ((cur.block << heads_shift) + head_l) * group;
-    const T* q = static_cast<const T*>(a.q) + cur.b * a.ld_q + static_cast<int64_t>(head0) * D;
+    const T* q = static_cast<const T*>(p.q) + cur.b * p.ld_q + static_cast<int64_t>(head0) * D;
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
       const bool on = 8 * n + g4 < group;
       const uint32_t* row = reinterpret_cast<const uint32_t*>(q + (on ? 8 * n + g4 : 0) * D);   // pairs of dims
-      zs[n][0] = zs[n][1] = a.scale2;
+      zs[n][0] = zs[n][1] = p.scale2;
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         if constexpr (!kE4M3) {
@@ -271,7 +271,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   uint32_t use = 0;
   bool ok = true;
   auto arrived = [&]() {   // the next slot's bytes are there
-    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(full + 8 * slot, use, a.status));
+    if (ok) ok = __all_sync(0xffffffffu, tc::mbar_wait(full + 8 * slot, use, p.status));
   };
   auto release = [&]() {
     __syncwarp();
@@ -412,14 +412,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           }
         }
     }
-    uint32_t p[kSub][kTiles][2];   // weights, 16 bits: at most 2^8, their sum kept in fp32
+    uint32_t wt[kSub][kTiles][2];   // weights, 16 bits: at most 2^8, their sum kept in fp32
 #pragma unroll
     for (int j = 0; j < kSub; ++j)
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-          p[j][n][r] = transposed(kPvF16 ? pack_f16(e[j][n][2 * r], e[j][n][2 * r + 1]) : pack_bf16(e[j][n][2 * r], e[j][n][2 * r + 1]));
+          wt[j][n][r] = transposed(kPvF16 ? pack_f16(e[j][n][2 * r], e[j][n][2 * r + 1]) : pack_bf16(e[j][n][2 * r], e[j][n][2 * r + 1]));
     if (partial) {   // rows that nobody sees may hold anything, and 0 x NaN is NaN
       constexpr int kUnits = S::kRowBytes / 16, kUnitsOf = S::kBlockBytes / 16;
       for (int i = lane; i < R * kUnits; i += 32) {
@@ -438,7 +438,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           uint32_t w[4];
           ldmatrix_x4_trans(w, (vb + v_off[j] + (i >> 2) * block_stride) ^ ((i & 3) * 32));
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, p[j][n][0], p[j][n][1]);
+          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, wt[j][n][0], wt[j][n][1]);
         }
       } else {
         // a word: dims 2 g4, 2 g4 + 1 of keys 2 t and 2 t + 1; the even dims are the tile's rows 0-7, the odd ones rows 8-15
@@ -451,7 +451,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
                                  e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4420))),
                                  e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4431)))};
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, p[j][n][0], p[j][n][1]);
+          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, wt[j][n][0], wt[j][n][1]);
         }
       }
     }
@@ -492,9 +492,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (strip == 0 && g4 == 0 && row < group) {
           const float lse2 = some ? m + log2f(l) : -INFINITY;
           if (from_start && to_end) {
-            if (a.lse != nullptr) a.lse[static_cast<int64_t>(cur.b) * a.H + ((cur.block << heads_shift) + head_l) * group + row] = lse2 / paged::kLog2e;
+            if (p.lse != nullptr) p.lse[static_cast<int64_t>(cur.b) * p.H + ((cur.block << heads_shift) + head_l) * group + row] = lse2 / paged::kLog2e;
           } else {
-            a.part_lse[(slot0 + (first ? 0 : 1)) * n_rows + head_l * group + row] = lse2;
+            p.part_lse[(slot0 + (first ? 0 : 1)) * n_rows + head_l * group + row] = lse2;
           }
         }
       }
@@ -536,10 +536,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         }
         if (from_start && to_end) {
           const int h = (cur.block << heads_shift) * group + rr;
-          uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + cur.b * a.ld_out + static_cast<int64_t>(h) * D + S::kMergeDims * chunk + d2);
+          uint32_t* out = reinterpret_cast<uint32_t*>(static_cast<T*>(p.out) + cur.b * p.ld_out + static_cast<int64_t>(h) * D + S::kMergeDims * chunk + d2);
           *out = kF16 ? pack_f16(sum.x, sum.y) : pack_bf16(sum.x, sum.y);
         } else {
-          *reinterpret_cast<float2*>(a.part_out + ((slot0 + (first ? 0 : 1)) * n_rows + rr) * D + S::kMergeDims * chunk + d2) = sum;
+          *reinterpret_cast<float2*>(p.part_out + ((slot0 + (first ? 0 : 1)) * n_rows + rr) * D + S::kMergeDims * chunk + d2) = sum;
         }
       }
       meet();
@@ -547,11 +547,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   };
 
   // sequences without tokens belong to no tile: their results, while the first tile is on its way
-  for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-    if (paged::seq_length(a, b, tid == 0) > 0) continue;
-    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + b * a.ld_out);
-    for (int i = tid; i < a.H * D / 8; i += 32 * kWarps) out[i] = make_uint4(0u, 0u, 0u, 0u);
-    for (int i = tid; i < a.H && a.lse != nullptr; i += 32 * kWarps) a.lse[static_cast<int64_t>(b) * a.H + i] = -INFINITY;
+  for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+    if (paged::seq_length(p, b, tid == 0) > 0) continue;
+    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(p.out) + b * p.ld_out);
+    for (int i = tid; i < p.H * D / 8; i += 32 * kWarps) out[i] = make_uint4(0u, 0u, 0u, 0u);
+    for (int i = tid; i < p.H && p.lse != nullptr; i += 32 * kWarps) p.lse[static_cast<int64_t>(b) * p.H + i] = -INFINITY;
   }
   bool from_start = cur.tile == 0, first = true;
   if (cur.left > 0) begin();
@@ -563,11 +563,11 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
       --cur.left;
       continue;
     }
-    if (cur.left == 1 && tid == 0) paged::say_parts(a, blockIdx.x, cur, from_start, first);
+    if (cur.left == 1 && tid == 0) paged::say_parts(p, blockIdx.x, cur, from_start, first);
     finish(from_start, last_of_seq, first);
     first = false;
     from_start = true;
-    paged::advance(a, cur, shift, blocks);
+    paged::advance(p, cur, shift, blocks);
     if (cur.left > 0) begin();
   }
 }

@@ -85,7 +85,7 @@ __device__ __forceinline__ uint64_t smem_desc_sw64(uint32_t addr, uint32_t sbo) 
 
 template <bool kF16>
 __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap q_map,
-                                                                   PagedAttnArgs a) {
+                                                                   PagedAttnArgs p) {
   extern __shared__ uint8_t smem_raw[];
   LatentSmem& sm = *reinterpret_cast<LatentSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -115,8 +115,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
   pdl_wait();
   pdl_launch_dependents();
   tc::fence_before_sync();
-  const bool raised = tc::status_raised(a.status);
-  Cursor cur = paged::first_entry(a, blockIdx.x, kShift, 1, lane);
+  const bool raised = tc::status_raised(p.status);
+  Cursor cur = paged::first_entry(p, blockIdx.x, kShift, 1, lane);
   const bool dead = __syncthreads_or(raised) != 0;   // the same in all threads, as in tc::block_gives_up
   tc::fence_after_sync();
   const uint32_t tmem_base = sm.tmem_slot;
@@ -125,16 +125,16 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
 
   if (warp == kCopyWarp) {
     // ================= copies =================
-    const int64_t n_rows = static_cast<int64_t>(max(a.n_pages, 1)) << a.page_shift;   // as the tensor map has them
+    const int64_t n_rows = static_cast<int64_t>(max(p.n_pages, 1)) << p.page_shift;   // as the tensor map has them
     auto row_of = [&]() -> int {   // cache row of the tile at the cursor; past the pool (rows of zeros) if its page is not one
       if (cur.left <= 0) return 0;
       const int s0 = cur.st.first_key(cur.tile, kShift);
-      const int p = a.page_table[cur.b * a.pt_stride + (s0 >> a.page_shift)];
-      if (p < 0 || p >= a.n_pages) {
-        if (lane == 0) paged::report_index(a.notice);
+      const int page = p.page_table[cur.b * p.pt_stride + (s0 >> p.page_shift)];
+      if (page < 0 || page >= p.n_pages) {
+        if (lane == 0) paged::report_index(p.notice);
         return static_cast<int>(n_rows);
       }
-      return (p << a.page_shift) + (s0 & ((1 << a.page_shift) - 1));
+      return (page << p.page_shift) + (s0 & ((1 << p.page_shift) - 1));
     };
     // Items of the ring, two slots each: Q of a sequence (heads 0-31, 32-63), then its tiles.
     int row = row_of(), pair = 0, issued = 0;
@@ -143,12 +143,12 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
     for (int g = 0; g < entries && alive; ++g) {
       const int this_row = row, b = cur.b;
       const bool q_first = fresh;
-      fresh = paged::advance(a, cur, kShift, 1);
+      fresh = paged::advance(p, cur, kShift, 1);
       row = row_of();   // (its page number is on its way while this tile waits for its slots)
       for (int item = q_first ? 0 : 1; item < 2 && alive; ++item) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          alive = alive && __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.k_empty[2 * pair + h]), use ^ 1u, a.status));
+          alive = alive && __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.k_empty[2 * pair + h]), use ^ 1u, p.status));
           if (!alive) break;
           if (tc::elect_one()) {
             const uint32_t full = smem_u32(&sm.k_full[2 * pair + h]), dst = smem_u32(sm.k[2 * pair + h]);
@@ -187,13 +187,13 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       };
       for (int g = 0; g < entries && ok; ++g) {
         if (fresh) {
-          if (!tc::mbar_wait(smem_u32(&sm.q_ready), piece++ & 1u, a.status)) break;
+          if (!tc::mbar_wait(smem_u32(&sm.q_ready), piece++ & 1u, p.status)) break;
           tc::mbar_arrive(smem_u32(&sm.k_empty[2 * pair + h]));   // Q has left its slots
           next();
         }
         const int buf = g & 1;
-        ok = tc::mbar_wait(smem_u32(&sm.k_full[2 * pair + h]), use, a.status) &&
-             tc::mbar_wait(smem_u32(&sm.s_free[2 * buf + h]), (static_cast<uint32_t>(g >> 1) & 1u) ^ 1u, a.status);
+        ok = tc::mbar_wait(smem_u32(&sm.k_full[2 * pair + h]), use, p.status) &&
+             tc::mbar_wait(smem_u32(&sm.s_free[2 * buf + h]), (static_cast<uint32_t>(g >> 1) & 1u) ^ 1u, p.status);
         if (!ok) break;
         tc::fence_after_sync();
         const uint64_t dk = tc::desc_advance(dk0, (2 * pair + h) * kSlotBytes);
@@ -209,18 +209,18 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
         }
         tc::umma_commit(smem_u32(&sm.s_full[2 * buf + h]));
         next();
-        fresh = paged::advance(a, cur, kShift, 1);
+        fresh = paged::advance(p, cur, kShift, 1);
       }
     }
   } else if (warp == kPvWarp) {
     // ================= O += P V =================
-    if (entries == 0 && lane == 0) a.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (entries == 0 && lane == 0) p.parts[blockIdx.x] = make_int4(0, 0, 0, 0);
     // sequences without tokens belong to no tile: their results, while the first tile is on its way
-    for (int b = blockIdx.x; b < a.batch; b += gridDim.x) {
-      if (paged::seq_length(a, b, lane == 0) > 0) continue;
-      uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + b * a.ld_out);
-      for (int i = lane; i < a.H * kDV / 8; i += 32) out[i] = make_uint4(0u, 0u, 0u, 0u);
-      for (int i = lane; i < a.H && a.lse != nullptr; i += 32) a.lse[static_cast<int64_t>(b) * a.H + i] = -INFINITY;
+    for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
+      if (paged::seq_length(p, b, lane == 0) > 0) continue;
+      uint4* out = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.out) + b * p.ld_out);
+      for (int i = lane; i < p.H * kDV / 8; i += 32) out[i] = make_uint4(0u, 0u, 0u, 0u);
+      for (int i = lane; i < p.H && p.lse != nullptr; i += 32) p.lse[static_cast<int64_t>(b) * p.H + i] = -INFINITY;
     }
     __syncwarp();
     if (tc::elect_one()) {
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       for (int g = 0; g < entries; ++g) {
         if (fresh && ++pair == kRing) pair = 0;   // (Q)
         // (given after O of the sequence before has been read out)
-        if (!tc::mbar_wait(smem_u32(&sm.p_ready[turn]), use, a.status)) break;
+        if (!tc::mbar_wait(smem_u32(&sm.p_ready[turn]), use, p.status)) break;
         tc::fence_after_sync();
         // the softmax warps give a sequence's last slots free: they may stage O there
         const bool last = cur.tile + 1 == cur.st.count || cur.left == 1;
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
           turn = 0;
           use ^= 1u;
         }
-        fresh = paged::advance(a, cur, kShift, 1);
+        fresh = paged::advance(p, cur, kShift, 1);
       }
     }
   } else {
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
     auto move_q = [&]() -> bool {
       const int row = 16 * quarter + (lane & 15), hi = lane >> 4, r = row & 31;
       const int at = 2 * pair + (quarter >> 1);
-      if (!__all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.k_full[at]), use, a.status))) return false;
+      if (!__all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.k_full[at]), use, p.status))) return false;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t w[32];
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       const int buf = g & 1;
       const int s0 = cur.st.first_key(cur.tile, kShift) + kHalfKeys * half;
       const bool partial = !cur.st.all_seen(s0, kHalfKeys);
-      ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.s_full[2 * buf + half]), static_cast<uint32_t>(g >> 1) & 1u, a.status));
+      ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.s_full[2 * buf + half]), static_cast<uint32_t>(g >> 1) & 1u, p.status));
       tc::fence_after_sync();
       float2 v[2 * kGroups];   // [group of eight keys j][row r] at 2 j + r: keys 8 j + 2 (lane % 4) + {0, 1} of the half
       {
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
         float x = fmaxf(v[r].x, v[r].y);
 #pragma unroll
         for (int j = 1; j < kGroups; ++j) x = fmaxf(x, fmaxf(v[2 * j + r].x, v[2 * j + r].y));
-        mx[r] = x * a.scale2;
+        mx[r] = x * p.scale2;
       }
       auto row_max = [&]() {
 #pragma unroll
@@ -372,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           const float ref = m_used[r] > -INFINITY ? m_used[r] : 0.f;   // (a row whose scores are all -inf weighs nothing)
-          const float2 scale = make_float2(a.scale2, a.scale2), minus = make_float2(-ref, -ref);
+          const float2 scale = make_float2(p.scale2, p.scale2), minus = make_float2(-ref, -ref);
           float2 sum2 = make_float2(0.f, 0.f);
 #pragma unroll
           for (int j = 0; j < kGroups; ++j) {
@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
           if (half == 0 && (lane & 3) == 0) sm.factor[row_s + 8 * r] = alpha;
         }
         const int before = turn == 0 ? kRing - 1 : turn - 1;   // (there is a tile before: a first one needs nothing)
-        ok = __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.pv_done[before]), turn == 0 ? turn_use ^ 1u : turn_use, a.status));
+        ok = __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.pv_done[before]), turn == 0 ? turn_use ^ 1u : turn_use, p.status));
         if (softmax_any(!ok)) break;
         tc::fence_after_sync();
         const float al = sm.factor[head_o];
@@ -448,8 +448,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       // ---- the sequence, or this unit's part of it, is done
       const bool whole = from_start && ends;
       const int b = cur.b;
-      if (cur.left == 1 && tid == 0) paged::say_parts(a, blockIdx.x, cur, from_start, first);
-      fresh = paged::advance(a, cur, kShift, 1);
+      if (cur.left == 1 && tid == 0) paged::say_parts(p, blockIdx.x, cur, from_start, first);
+      fresh = paged::advance(p, cur, kShift, 1);
       if (cur.left > 0) ok = move_q();   // every Q K^T of the old one is complete
 #pragma unroll
       for (int r = 0; r < 2; ++r) {
@@ -466,19 +466,19 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
           const bool some = l > 0.f || l != l;
           const float lse2 = some ? m_used[r] + log2f(l) : -INFINITY;
           sm.factor[row] = some ? 1.f / l : 0.f;
-          if (row < a.H) {
-            if (!whole) a.part_lse[(2 * blockIdx.x + (first ? 0 : 1)) * kHeads + row] = lse2;
-            else if (a.lse != nullptr) a.lse[static_cast<int64_t>(b) * a.H + row] = lse2 / paged::kLog2e;
+          if (row < p.H) {
+            if (!whole) p.part_lse[(2 * blockIdx.x + (first ? 0 : 1)) * kHeads + row] = lse2;
+            else if (p.lse != nullptr) p.lse[static_cast<int64_t>(b) * p.H + row] = lse2 / paged::kLog2e;
           }
         }
       }
-      ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.pv_done[this_turn]), this_use, a.status));
+      ok = ok && __all_sync(0xffffffffu, tc::mbar_wait(smem_u32(&sm.pv_done[this_turn]), this_use, p.status));
       if (softmax_any(!ok)) break;
       tc::fence_after_sync();
       const float inv = sm.factor[head_o];
       const int dim0 = 256 * half + 128 * half_o;
       uint8_t* stage = &sm.k[2 * this_pair][0][0];   // whole results: rows of 1024 bytes, 16-byte units XORed with the row, over two slots
-      float* part = a.part_out + ((2 * static_cast<int64_t>(blockIdx.x) + (first ? 0 : 1)) * kDV + dim0) * kHeads + 4 * head_o;
+      float* part = p.part_out + ((2 * static_cast<int64_t>(blockIdx.x) + (first ? 0 : 1)) * kDV + dim0) * kHeads + 4 * head_o;
 #pragma unroll 1
       for (int c = 0; c < 128; c += 32) {
         uint32_t o[32];
@@ -503,8 +503,8 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       tc::fence_before_sync();   // O has been read: the next sequence's P V may begin once its first P is there
       softmax_sync();            // (and the factors have been read)
       if (whole) {
-        uint16_t* out = static_cast<uint16_t*>(a.out) + b * a.ld_out;
-        for (int i = tid; i < a.H * (kDV / 8); i += kSoftmaxThreads) {
+        uint16_t* out = static_cast<uint16_t*>(p.out) + b * p.ld_out;
+        for (int i = tid; i < p.H * (kDV / 8); i += kSoftmaxThreads) {
           const int row = i >> 6, u = i & 63;
           *reinterpret_cast<uint4*>(out + 8 * i) = *reinterpret_cast<const uint4*>(stage + row * 1024 + ((u ^ (row & 7)) << 4));
         }
