@@ -162,18 +162,17 @@ def kv_workspace_bytes(kv: LsaKvParams) -> int:
     return out.value
 
 
-def _kv_rows(t, width: int, dtype, where: str, rows: int | None = None):
-    """(pointer, elements from one row to the next) of rows of `width` elements, given as [rows, width] or [rows, heads, dims]."""
+def _kv_rows(t, width: int, dtype, where: str, rows: int):
+    """(pointer, elements from one row to the next) of `rows` rows of `width` elements, given as [rows, width] or [rows, heads, dims]."""
     if t is None:
         return None, 0
-    n = t.size(0)
-    if t.dtype is dtype and t.is_contiguous() and t.numel() == n * width and (rows is None or n == rows):   # (most calls end here)
+    if t.dtype is dtype and t.is_contiguous() and t.numel() == rows * width:   # (most calls end here)
         return t.data_ptr(), width
     st, sh = t.stride(), t.shape
     inner = len(sh) >= 2 and st[-1] == 1 and (len(sh) == 2 or (len(sh) == 3 and (sh[1] == 1 or st[1] == sh[2])))
-    if not inner or t.dtype is not dtype or (sh[1] if len(sh) == 2 else sh[1] * sh[2]) != width or (rows is not None and n != rows):
-        raise LsaError(-1, where, f"rows of {width} {dtype} wanted{'' if rows is None else f', {rows} of them'}: got {tuple(sh)} {t.dtype}, strides {st}")
-    return t.data_ptr(), (st[0] if n > 1 else max(st[0], width))
+    if not inner or t.dtype is not dtype or (sh[1] if len(sh) == 2 else sh[1] * sh[2]) != width or sh[0] != rows:
+        raise LsaError(-1, where, f"{rows} rows of {width} {dtype} wanted: got {tuple(sh)} {t.dtype}, strides {st}")
+    return t.data_ptr(), (st[0] if rows > 1 else max(st[0], width))
 
 
 def _kv_flat(t, dtype, count: int, where: str):
@@ -340,31 +339,36 @@ class Context:
         """The arguments of a cache: pools as [rows, heads * dims] or [rows, heads, dims], scales as [rows, heads]."""
         if self.kv is None:
             raise LsaError(-1, where, "the context was made without kv parameters")
-        rows, batch = k_pool.size(0), page_table.size(0)
+        # (a look at a tensor's shape costs more than its number of elements)
+        rows = k_pool.numel() // self._kv_wk if k_pool.is_contiguous() else k_pool.shape[0]
         n_pages, rest = divmod(rows, self._kv_page)
         if rest:
             raise LsaError(-1, where, f"a pool of {rows} rows is not a whole number of pages of {self._kv_page}")
-        if page_table.dtype is not torch.int32 or page_table.dim() != 2 or page_table.stride(1) != 1:
+        sh = page_table.shape
+        if page_table.dtype is not torch.int32 or len(sh) != 2 or not (page_table.is_contiguous() or page_table.stride(1) == 1):
             raise LsaError(-1, where, "page_table: int32 [batch, pages] with contiguous rows wanted")
+        batch, pitch = sh
+        if batch > 1 and not page_table.is_contiguous():
+            pitch = page_table.stride(0)
         cached = self._kv_codes.get(k_pool.dtype, torch.uint8) if self._kv_codes else self._kv_dtype
-        k, ld_k = _kv_rows(k_pool, self._kv_wk, cached, where)
+        k, ld_k = _kv_rows(k_pool, self._kv_wk, cached, where, rows)
         v, ld_v = _kv_rows(v_pool, self._kv_wv, cached, where, rows)
         ks, vs = (None, None) if k_scale is None and v_scale is None else (_kv_flat(x, torch.float32, rows * self.kv.n_kv_heads, where) for x in (k_scale, v_scale))
-        return (k, ld_k, v, ld_v, ks, vs, n_pages, page_table.data_ptr(), page_table.stride(0) if batch > 1 else page_table.size(1),
-                _kv_flat(ctx_len, torch.int32, batch, where), batch)
+        return (k, ld_k, v, ld_v, ks, vs, n_pages, page_table.data_ptr(), pitch, _kv_flat(ctx_len, torch.int32, batch, where), batch)
 
     def kv_append(self, k_new, v_new, k_pool, v_pool, page_table, ctx_len, ctx_len_out=None, tok_start=None, q=None, q_out=None,
                   cos_sin=None, k_scale=None, v_scale=None):
         """lsa_kv_append: new tokens [n_tok, heads, dims] into the cache, rotated; q (optional) rotated into q_out."""
         where = "lsa_kv_append"
         cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where)
-        batch, n_tok, n_pos, dtype = cache[-1], k_new.size(0), 0, self._kv_dtype
+        batch, dtype, n_pos = cache[-1], self._kv_dtype, 0
+        n_tok = k_new.numel() // self._kv_wk if k_new.is_contiguous() else k_new.shape[0]
         if cos_sin is not None:
-            n_pos = cos_sin.size(0)
-            if cos_sin.dim() != 2 or cos_sin.size(1) != self._kv_rope:
+            n_pos, width = cos_sin.shape if cos_sin.dim() == 2 else (0, -1)
+            if width != self._kv_rope:
                 raise LsaError(-1, where, f"cos_sin: [positions, {self._kv_rope}] wanted, got {tuple(cos_sin.shape)}")
         self._chk(lib().lsa_kv_append(
-            self.h, self._kv_ref, *_kv_rows(k_new, self._kv_wk, dtype, "k_new"), *_kv_rows(v_new, self._kv_wv, dtype, "v_new", n_tok),
+            self.h, self._kv_ref, *_kv_rows(k_new, self._kv_wk, dtype, "k_new", n_tok), *_kv_rows(v_new, self._kv_wv, dtype, "v_new", n_tok),
             *_kv_rows(q, self._kv_wq, dtype, "q", n_tok), *_kv_rows(q_out, self._kv_wq, dtype, "q_out", n_tok), n_tok,
             _kv_flat(tok_start, torch.int32, batch + 1, "tok_start"), _kv_flat(cos_sin, torch.float32, n_pos * self._kv_rope, "cos_sin"), n_pos,
             *cache, _kv_flat(ctx_len_out, torch.int32, batch, "ctx_len_out")), where)

@@ -155,12 +155,12 @@ def test_kinds_of_cache_and_their_pointers():
 def test_binding_refuses_tensors_of_another_form():
     """The binding's own checks, which need no library call."""
     x = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
-    assert binding._kv_rows(x, 1024, torch.bfloat16, "x")[1] == 1024
+    assert binding._kv_rows(x, 1024, torch.bfloat16, "x", 6)[1] == 1024
     wide = torch.zeros(6, 20, 128, dtype=torch.bfloat16)
-    assert binding._kv_rows(wide[:, 4:12], 1024, torch.bfloat16, "x")[1] == 2560
-    for bad in (x.float(), x[:, :4], x[:, ::2], x[..., ::2], x.transpose(0, 1)):
+    assert binding._kv_rows(wide[:, 4:12], 1024, torch.bfloat16, "x", 6)[1] == 2560
+    for bad in (x.float(), x[:5], x[:, :4], x[:, ::2], x[..., ::2], x.transpose(0, 1)):
         with pytest.raises(binding.LsaError) as e:
-            binding._kv_rows(bad, 1024, torch.bfloat16, "x")
+            binding._kv_rows(bad, 1024, torch.bfloat16, "x", 6)
         assert e.value.code == -1
     with pytest.raises(binding.LsaError):
         binding._kv_flat(torch.zeros(4, dtype=torch.int64), torch.int32, 4, "n")
