@@ -13,6 +13,14 @@ namespace paged {
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// Weights are 2^(score - reference), and a head's reference is moved only when its maximum has grown by more than 2^8, so that the
+// output is rarely rescaled: a weight is at most 2^8 where the reference was the maximum.  fp16 weights end at 2^-24, and a long
+// sequence may have its mass in hundreds of thousands of weights smaller than that beside one of 1, so their reference lies 2^7 below
+// the maximum: weights of at most 2^15, and down to 2^-32 of the largest.  (bf16 has the range of fp32.)
+constexpr float kRescaleGap = 8.f;
+template <bool kF16Weights>
+constexpr float kLift = kF16Weights ? 7.f : 0.f;
+
 // A number of the caller's that points outside its array: recorded in the notice word (see lsa_status), never followed.
 __device__ __forceinline__ void report_index(int* notice) { report_status(notice, kDevBadIndex); }
 

@@ -27,7 +27,6 @@ using paged::exp2_fast;
 
 constexpr int kWarps = 8, kThreads = 32 * (kWarps + 1);   // and the one that copies
 constexpr int kRing = 6;
-constexpr float kRescaleGap = 8.f;   // the output is rescaled only when a head's maximum grows by more than 2^8
 
 // kTiles: groups of eight query heads per KV head (1 or 2).
 template <int D, bool kE4M3, int kTiles>
@@ -85,12 +84,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   using S = Shape<D, kE4M3, kTiles>;
   constexpr bool kF16 = !__is_same(T, __nv_bfloat16);
   constexpr bool kQkF16 = kF16 || kE4M3, kPvF16 = kF16 && !kE4M3;
+  constexpr float kGap = paged::kRescaleGap + paged::kLift<kPvF16>;
   constexpr int R = S::kRows, kSub = R / 16, kHeadsOf = 8 * kTiles;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   float* const scales = reinterpret_cast<float*>(ring + kRing * S::kBytes);     // [slot][row of the tile][head]
   float* const merge = scales + kRing * S::kScales / 4;
-  float2* const ml = reinterpret_cast<float2*>(merge + S::kMerge / 4);          // {maximum, sum} per warp and head
+  float2* const ml = reinterpret_cast<float2*>(merge + S::kMerge / 4);          // {reference, sum} per warp and head
   const uint32_t full = smem_u32(ml + kWarps * kHeadsOf), empty = full + 8 * kRing;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   const int strip_shift = 3 - heads_shift, n_strips = 1 << strip_shift;
@@ -210,7 +210,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     k_off[0] = v_off[0] = strip_at(lane) + twist(lane);
   }
 
-  // ---- the state of a (sequence, block): query fragments, output, maxima and sums of the heads 8 n + 2 t4, + 1
+  // ---- the state of a (sequence, block): query fragments, output, references and sums of the heads 8 n + 2 t4, + 1
   uint32_t qf[kTiles][D / 16][2];
   float o[kTiles][D / 16][4];
   float zs[kTiles][2], m_used[kTiles][2], l_run[kTiles][2];
@@ -349,7 +349,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             for (int n = 0; n < kTiles; ++n) s[j][n][2 * r] = s[j][n][2 * r + 1] = -INFINITY;
           }
     }
-    // P with the maxima as they are; only where a head has grown too far is its maximum moved before
+    // P with the references as they are; only where a head has grown too far is its reference moved before
     float mx[kTiles][2];
     bool need = false;
 #pragma unroll
@@ -360,7 +360,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
         for (int j = 1; j < kSub; ++j) x = fmaxf(x, fmaxf(s[j][n][c], s[j][n][2 + c]));
         mx[n][c] = x * zs[n][c];
-        need = need || mx[n][c] > m_used[n][c] + kRescaleGap;
+        need = need || mx[n][c] > m_used[n][c] + kGap;
       }
     if (__any_sync(0xffffffffu, need)) {
 #pragma unroll
@@ -370,9 +370,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           float x = mx[n][c];
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-          if (x > m_used[n][c] + kRescaleGap) {
-            const float al = exp2_fast(m_used[n][c] - x);   // (the first time: 0)
-            m_used[n][c] = x;
+          if (x > m_used[n][c] + kGap) {
+            const float to = x - paged::kLift<kPvF16>, al = exp2_fast(m_used[n][c] - to);   // (the first time: 0)
+            m_used[n][c] = to;
             l_run[n][c] *= al;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
@@ -385,7 +385,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     float e[kSub][kTiles][4];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      // (a head whose scores are all -inf so far has no maximum: its weights are 0)
+      // (a head whose scores are all -inf so far has no reference: its weights are 0)
       const float ref[2] = {m_used[n][0] > -INFINITY ? m_used[n][0] : 0.f, m_used[n][1] > -INFINITY ? m_used[n][1] : 0.f};
 #pragma unroll
       for (int j = 0; j < kSub; ++j)
@@ -412,7 +412,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           }
         }
     }
-    uint32_t wt[kSub][kTiles][2];   // weights, 16 bits: at most 2^8, their sum kept in fp32
+    uint32_t wt[kSub][kTiles][2];   // weights in 16 bits; their sum is that of the unrounded ones
 #pragma unroll
     for (int j = 0; j < kSub; ++j)
 #pragma unroll

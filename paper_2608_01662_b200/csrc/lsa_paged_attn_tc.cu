@@ -40,7 +40,6 @@ constexpr int kRing = 3;                                            // tiles, tw
 constexpr int kSoftmaxWarps = 8, kCopyWarp = 8, kQkWarp = 9, kPvWarp = 11, kThreads = 384;
 constexpr int kSoftmaxThreads = 32 * kSoftmaxWarps;
 constexpr uint32_t kTmemCols = 512, kColQ = 256, kColS = 384, kSBuf = 64;
-constexpr float kRescaleGap = 8.f;   // O is rescaled only when a row's maximum grows by more than 2^8
 
 struct LatentSmem {
   alignas(1024) uint8_t k[2 * kRing][kAtoms][kAtomBytes];
@@ -88,6 +87,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
                                                                    PagedAttnArgs p) {
   extern __shared__ uint8_t smem_raw[];
   LatentSmem& sm = *reinterpret_cast<LatentSmem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  constexpr float kLift = paged::kLift<kF16>, kGap = paged::kRescaleGap + kLift;
   const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
 
   if (tid == 0) {
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       next_item();
       return true;
     };
-    float m_used[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};   // of rows row_s and row_s + 8, in log2 units; the thread's share of the sums
+    float m_used[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};   // references of rows row_s and row_s + 8, in log2 units; the thread's share of their sums
     bool ok = true, fresh = true, from_start = cur.tile == 0, first = true;
     if (entries > 0) ok = move_q();
     for (int g = 0; g < entries; ++g) {
@@ -360,11 +360,11 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
       bool need = false;
       if (fresh) {
         row_max();
-        m_used[0] = mx[0];
-        m_used[1] = mx[1];
+        m_used[0] = mx[0] - kLift;
+        m_used[1] = mx[1] - kLift;
         l_run[0] = l_run[1] = 0.f;
       } else {
-        need = mx[0] > m_used[0] + kRescaleGap || mx[1] > m_used[1] + kRescaleGap;
+        need = mx[0] > m_used[0] + kGap || mx[1] > m_used[1] + kGap;
       }
       float sum[2];
       auto work_out_p = [&]() {
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
             e.x = exp2_fast(e.x);
             e.y = exp2_fast(e.y);
             sum2 = add2(sum2, e);
-            pk[j][r] = pack2<kF16>(e.x, e.y);   // 16 bits of a weight of at most 2^8; the sum is of the unrounded ones
+            pk[j][r] = pack2<kF16>(e.x, e.y);   // the sum is of the unrounded ones
           }
           sum[r] = sum2.x + sum2.y;
         }
@@ -399,9 +399,9 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
           float alpha = 1.f;
-          if (mx[r] > m_used[r] + kRescaleGap) {
-            alpha = exp2_fast(m_used[r] - mx[r]);
-            m_used[r] = mx[r];
+          if (mx[r] > m_used[r] + kGap) {
+            alpha = exp2_fast(m_used[r] - (mx[r] - kLift));
+            m_used[r] = mx[r] - kLift;
           }
           l_run[r] *= alpha;
           if (half == 0 && (lane & 3) == 0) sm.factor[row_s + 8 * r] = alpha;

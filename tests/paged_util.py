@@ -94,6 +94,24 @@ class Cache:
         return (k, k[..., :self.dv]) if self.latent else (k, real(self.v, self.v_scale, self.dv))
 
 
+def many_small_weights(shape, page, device):
+    """fp16 sequences of 4096 tokens whose first weighs 1 and has no value, the others 2^-26 each with values of 2^10."""
+    c = Cache([4096] * 40, shape, page, "fp16", False, device, seed=21)
+    c.q[:] = 0
+    c.q[..., 0] = 1
+    c.k[:] = 0
+    if c.v is None:
+        c.k[:, 1:512] = 1024
+    else:
+        c.v[:] = 1024
+    first = torch.from_numpy(c.table[:, 0].astype(np.int64) * page).to(device)
+    c.k[first] = 0
+    c.k[first, ::c.d] = 26 * math.log(2) * c.d ** 0.5
+    if c.v is not None:
+        c.v[first] = 0
+    return c
+
+
 def attend(cache, ctx=None, out=None, lse=None, **kw):
     ctx = ctx or binding.Context(None, 0, 0, len(cache.lengths), device=cache.device, kv=cache.params(**kw))
     B = len(cache.lengths)
@@ -107,8 +125,8 @@ def check_attend(cache, out, lse, sink=0, window=0, sequences=None):
     """Every element against the oracle, within what the roundings of the method allow.
 
     With u_p the rounding of a weight to 16 bits (bf16 where the cache is e4m3), u_o that of the result, and weights p, values v:
-      |out - ref| <= (u_p + 2 e) sum_s p_s |v_s| + u_o |ref|   (+ 2^-25 sum_s |v_s| where weights are fp16: a weight below 2^-14
-    is rounded to a multiple of 2^-24; the largest weight of a part is at least 1 before the division)
+      |out - ref| <= (u_p + 2 e) sum_s p_s |v_s| + u_o |ref|   (+ 2^-32 sum_s |v_s| where weights are fp16: a weight below 2^-14
+    is rounded to a multiple of 2^-24; the largest weight of a part is at least 2^7 before the division)
     where e is the relative error of a weight before that rounding: that of its score, (d + 8) roundings of fp32 of products whose
     absolute sum is at most sum_i |q_i k_i| (a tree or a chain of fp32 additions, in log2 units, times ln 2), 2^-21 for exp2 and
     (n / 8 + 512) roundings for the chains of sums.  The log-sum-exp carries the score's error and the sum's.
@@ -138,7 +156,7 @@ def check_attend(cache, out, lse, sink=0, window=0, sequences=None):
             e = e_z + 2.0 ** -21 + (len(pos) / 8 + 512) * 2.0 ** -24
             tol = (u_p + 2 * e) * mass + u_o * np.abs(ref[h]) * (1 + u_p)
             if cache.dtype == "fp16" and not cache.e4m3:
-                tol = tol + 2.0 ** -25 * np.abs(v[rows, g]).sum(0)
+                tol = tol + 2.0 ** -32 * np.abs(v[rows, g]).sum(0)
             if cache.dtype == "fp16":
                 tol = tol + 2.0 ** -25   # a result below 2^-14 is rounded to a multiple of 2^-24
             err = np.abs(got[b, h] - ref[h])

@@ -259,3 +259,10 @@ def test_no_sequences(cuda_device):
     before = ctx.launch_count()
     ctx.paged_attn(e, pool, pool, torch.zeros(0, 3, dtype=torch.int32, device=cuda_device), torch.zeros(0, dtype=torch.int32, device=cuda_device), e)
     assert ctx.launch_count() == before and ctx.status() == 0
+
+
+def test_many_small_weights(cuda_device):
+    c = pu.many_small_weights((8, 8, 64, 64), 16, cuda_device)
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse, sequences=[0, 7, 39])

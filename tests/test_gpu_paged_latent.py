@@ -196,3 +196,10 @@ def test_dense_and_sparse_attention_of_the_same_cache(cuda_device):
     assert ctx.status() == 0
     # both within bf16 weights and one rounding of the same sums: two times (2 u) of the mass, whose mean |v| is below 1
     assert float((out.double() - wl.out[0].double()).abs().max()) <= 4 * 2.0 ** -8
+
+
+def test_many_small_weights(cuda_device):
+    c = pu.many_small_weights((64, 1, 576, 512), 64, cuda_device)
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse, sequences=[0, 7, 39])
