@@ -410,7 +410,7 @@ LSA_API int lsa_kv_workspace_bytes(const lsa_kv_params* p, size_t* bytes);
  *              tok_start[0] .. tok_start[batch] - 1 are padding and are neither read for their values nor written
  *   cos_sin    fp32 [n_pos, d_rope]: the cosines, then the sines, of position pos's d_rope / 2 angles; NULL iff d_rope = 0
  *   k_pool, v_pool   [n_pages * kv_page] rows of ld_k / ld_v elements; v_pool NULL for latent caches
- *   k_scale, v_scale  fp32 [n_pages * kv_page, n_kv_heads], e4m3 caches only: written with the codes.  Scale = amax / 448 of
+ *   k_scale, v_scale  fp32 [n_pages * kv_page, n_kv_heads], 16-byte aligned, e4m3 caches only: written with the codes.  Scale = amax / 448 of
  *              the head's rotated fp32 values (1 for a zero row), code = round-to-nearest-even of value / scale, saturating
  *   page_table int32 [batch, page_table_stride]; every page that the new tokens reach must be in it
  *   ctx_len    int32 [batch]: lengths BEFORE the call.  ctx_len_out: optional int32 [batch], the lengths after it; may be

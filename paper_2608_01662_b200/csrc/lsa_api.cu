@@ -874,6 +874,7 @@ static int check_kv_cache(const lsa_kv_params* p, const void* k_pool, int64_t ld
   if (ld_k < static_cast<int64_t>(p->n_kv_heads) * p->d_qk || ld_k % unit != 0 || !aligned16(k_pool)) return LSA_ERR_SHAPE;
   if (!p->latent && (ld_v < static_cast<int64_t>(p->n_kv_heads) * p->d_v || ld_v % unit != 0 || !aligned16(v_pool))) return LSA_ERR_SHAPE;
   if (ld_k > (1ll << 31) || (!p->latent && ld_v > (1ll << 31))) return LSA_ERR_SHAPE;
+  if (!aligned16(k_scale) || !aligned16(v_scale)) return LSA_ERR_SHAPE;   // (the scales of four heads are fetched at once)
   // rows and positions are 32-bit numbers in the kernels
   constexpr int64_t kMost = (1ll << 31) - 1024;
   if (n_pages > kMost / p->kv_page || page_table_stride > kMost / p->kv_page) return LSA_ERR_SHAPE;

@@ -148,6 +148,8 @@ def test_kinds_of_cache_and_their_pointers():
     assert _attn(e4m3) == -1 and _attn(e4m3, ks=A) == -1               # codes come with both scales
     assert _attn(e4m3, ks=A, vs=A, ld_k=1024 + 8) == -2                # 16 codes are 16 bytes
     assert _attn(e4m3, ks=A, vs=A, v=A + 8) == -2
+    for scales in (dict(ks=A + 4, vs=A), dict(ks=A, vs=A + 8)):        # those of four heads are fetched at once
+        assert _attn(e4m3, **scales) == -2 and _append(e4m3, **scales) == -2
     assert _append(mla, vn=A) == -1 and _append(gqa, vn=0) == -1 and _append(gqa, cs=A) == -1
     assert _append(gqa, ld_vn=1000) == -2 and _append(gqa, v=A + 8) == -2 and _append(gqa, vn=A + 8) == -2
 
