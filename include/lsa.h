@@ -413,11 +413,11 @@ LSA_API int lsa_kv_workspace_bytes(const lsa_kv_params* p, size_t* bytes);
  *   k_scale, v_scale  fp32 [n_pages * kv_page, n_kv_heads], 16-byte aligned, e4m3 caches only: written with the codes.  Scale = amax / 448 of
  *              the head's rotated fp32 values (1 for a zero row), code = round-to-nearest-even of value / scale, saturating
  *   page_table int32 [batch, page_table_stride]; every page that the new tokens reach must be in it
- *   ctx_len    int32 [batch]: lengths BEFORE the call.  ctx_len_out: optional int32 [batch], the lengths after it; may be
- *              ctx_len itself
+ *   ctx_len    int32 [batch]: lengths BEFORE the call.  ctx_len_out: optional int32 [batch], the lengths after it (tokens that
+ *              found no place are counted too); may be ctx_len itself, else the two do not overlap
  * A length below 0, a position outside the table or the angles, or a page number outside [0, n_pages) leaves that token's
  * outputs as they were and is reported as LSA_ERR_INDEX by lsa_status; the other tokens are served.  Two tokens of a call must not
- * share a row.  One launch (two where tok_start is given and ctx_len_out overlaps ctx_len). */
+ * share a row.  One launch (two where tok_start is given and ctx_len_out is ctx_len, or there are no tokens). */
 LSA_API int lsa_kv_append(lsa_ctx* ctx, const lsa_kv_params* p, const void* k_new, int64_t ld_k_new, const void* v_new,
                           int64_t ld_v_new, const void* q, int64_t ld_q, void* q_out, int64_t ld_q_out, int64_t n_tok,
                           const int32_t* tok_start, const float* cos_sin, int64_t n_pos, void* k_pool, int64_t ld_k,

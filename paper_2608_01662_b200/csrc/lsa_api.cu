@@ -925,6 +925,10 @@ int lsa_kv_append(lsa_ctx* c, const lsa_kv_params* p, const void* k_new, int64_t
   if (!rows_ok(k_new, ld_k_new, wk) || !rows_ok(v_new, ld_v_new, wk) || !rows_ok(q, ld_q, wq) || !rows_ok(q_out, ld_q_out, wq)) return LSA_ERR_SHAPE;
   if (q != nullptr && q == q_out && ld_q != ld_q_out) return LSA_ERR_ARG;
   if (cos_sin != nullptr && !aligned16(cos_sin)) return LSA_ERR_SHAPE;
+  if (ctx_len_out != nullptr && ctx_len_out != ctx_len) {   // (a block would read another's new length)
+    const uintptr_t in = reinterpret_cast<uintptr_t>(ctx_len), out = reinterpret_cast<uintptr_t>(ctx_len_out);
+    if ((in < out ? out - in : in - out) < static_cast<uintptr_t>(batch) * sizeof(int32_t)) return LSA_ERR_ARG;
+  }
   if (c == nullptr) return LSA_ERR_ARG;   // (last: the arguments are judged without a device)
   if (batch == 0) return LSA_OK;
   if (n_tok == 0 && ctx_len_out == nullptr) return LSA_OK;

@@ -297,8 +297,7 @@ cudaError_t launch_d(const KvAppendArgs& a, cudaStream_t st) {
 cudaError_t launch_kv_append(const KvAppendArgs& args, cudaStream_t st, int64_t* n_launch) {
   KvAppendArgs a = args;
   // with several tokens a sequence its length is read by several blocks
-  const uintptr_t in = reinterpret_cast<uintptr_t>(a.ctx_len), out = reinterpret_cast<uintptr_t>(a.ctx_len_out), bytes = static_cast<uintptr_t>(a.batch) * 4;
-  const bool later = a.tok_start != nullptr && a.ctx_len_out != nullptr && (a.n_tok == 0 || (in < out + bytes && out < in + bytes));
+  const bool later = a.tok_start != nullptr && a.ctx_len_out != nullptr && (a.n_tok == 0 || a.ctx_len_out == a.ctx_len);
   if (later) a.ctx_len_out = nullptr;
   cudaError_t e = cudaSuccess;
   if (a.n_tok > 0) {

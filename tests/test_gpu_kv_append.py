@@ -183,6 +183,20 @@ def test_in_place(cuda_device, decode):
         assert ctx.status() == 0 and lens.tolist() == lengths and torch.equal(q, q_first) and torch.equal(c.k, k_first)
 
 
+@pytest.mark.parametrize("decode", [True, False])
+def test_lengths_that_overlap_in_part_are_refused(cuda_device, decode):
+    c, t, old = make((8, 2, 64, 64), [9, 64, 300], [1, 1, 1], 64, "bf16", False, cuda_device, decode, 32, 0, False, seed=6)
+    ctx = t.append()
+    both = torch.zeros(7, dtype=torch.int32, device=cuda_device)
+    for out in (both[1:4], both[3:6]):
+        with pytest.raises(binding.LsaError) as e:
+            t.append(ctx, ctx_len=both[2:5], ctx_len_out=out)
+        assert e.value.code == -1
+    both[3:6] = t.before
+    t.append(ctx, ctx_len=both[3:6], ctx_len_out=both[0:3])
+    assert ctx.status() == 0 and both[:3].tolist() == [9, 64, 300]
+
+
 def test_no_queries_no_lengths_no_tokens(cuda_device):
     c, t, old = make((8, 2, 64, 64), [3, 20], [3, 4], 16, "bf16", False, cuda_device, False, 32, 0, False, seed=7)
     ctx = t.append()
