@@ -162,26 +162,47 @@ def kv_workspace_bytes(kv: LsaKvParams) -> int:
     return out.value
 
 
-def _kv_rows(t, width: int, dtype, where: str, rows: int):
-    """(pointer, elements from one row to the next) of `rows` rows of `width` elements, given as [rows, width] or [rows, heads, dims]."""
+def _kv_rows(t, heads: int, dims: int, dtype, where: str, rows: int, device: int = -1):
+    """(pointer, elements from one row to the next) of rows of heads * dims elements, given as [rows, heads, dims] or [rows, heads * dims]
+    on the device of that number (-1: the host)."""
     if t is None:
         return None, 0
-    if t.dtype is dtype and t.is_contiguous() and t.numel() == rows * width:   # (most calls end here)
-        return t.data_ptr(), width
-    st, sh = t.stride(), t.shape
-    inner = len(sh) >= 2 and st[-1] == 1 and (len(sh) == 2 or (len(sh) == 3 and (sh[1] == 1 or st[1] == sh[2])))
-    if not inner or t.dtype is not dtype or (sh[1] if len(sh) == 2 else sh[1] * sh[2]) != width or sh[0] != rows:
-        raise LsaError(-1, where, f"{rows} rows of {width} {dtype} wanted: got {tuple(sh)} {t.dtype}, strides {st}")
-    return t.data_ptr(), (st[0] if rows > 1 else max(st[0], width))
+    if t.dtype is dtype and t.shape == (rows, heads, dims) and t.get_device() == device and t.is_contiguous():   # (most calls end here)
+        return t.data_ptr(), heads * dims
+    st, sh = t.stride(), tuple(t.shape)
+    if t.get_device() != device:
+        raise LsaError(-1, where, f"a tensor on {t.device}: another device than the context's")
+    inner = (sh == (rows, heads, dims) and (heads == 1 or st[1] == dims)) or sh == (rows, heads * dims)
+    if not inner or st[-1] != 1 or t.dtype is not dtype:
+        raise LsaError(-1, where, f"{rows} rows of {heads} heads of {dims} {dtype} wanted: got {sh} {t.dtype}, strides {st}")
+    return t.data_ptr(), (st[0] if rows > 1 else max(st[0], heads * dims))
 
 
-def _kv_flat(t, dtype, count: int, where: str):
+def _kv_flat(t, dtype, count: int, where: str, device: int = -1):
     """Pointer to a contiguous array of `count` elements."""
     if t is None:
         return None
+    if t.get_device() != device:
+        raise LsaError(-1, where, f"a tensor on {t.device}: another device than the context's")
     if t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
         raise LsaError(-1, where, f"{count} contiguous {dtype} wanted: got {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
+
+
+def _kv_table(t, where: str, device: int = -1):
+    """(rows, entries from one row to the next, pointer) of a page table.  A row's length limit is its pitch: all of the last one has to
+    lie in the tensor's memory, which it may not in a view of some columns."""
+    sh = t.shape
+    if t.dtype is not torch.int32 or len(sh) != 2 or t.get_device() != device:
+        raise LsaError(-1, where, f"page_table: int32 [batch, pages] on the context's device wanted, got {tuple(sh)} {t.dtype} on {t.device}")
+    if sh[0] <= 1 or t.is_contiguous():
+        if sh[1] > 1 and t.stride(1) != 1:
+            raise LsaError(-1, where, "page_table: contiguous rows wanted")
+        return sh[0], sh[1], t.data_ptr()
+    pitch = t.stride(0)
+    if t.stride(1) != 1 or pitch < sh[1] or 4 * (t.storage_offset() + sh[0] * pitch) > t.untyped_storage().nbytes():
+        raise LsaError(-1, where, f"page_table: contiguous rows wanted, the last one's whole pitch in memory; strides {t.stride()}")
+    return sh[0], pitch, t.data_ptr()
 
 
 STATIC_SCRATCH_BYTES = 8 << 20
@@ -224,8 +245,8 @@ class Context:
             self._kv_ref, self._kv_page, self._kv_rope = ctypes.byref(kv), kv.kv_page, kv.d_rope
             self._kv_dtype = tuple(_KV_DTYPES.values())[kv.dtype]
             self._kv_codes = {torch.float8_e4m3fn: torch.float8_e4m3fn} if kv.cache_e4m3 else None   # (else bytes)
-            self._kv_wk, self._kv_wv = kv.n_kv_heads * kv.d_qk, kv.n_kv_heads * kv.d_v
-            self._kv_wq, self._kv_wo = kv.n_heads * kv.d_qk, kv.n_heads * kv.d_v
+            self._kv_k, self._kv_v, self._kv_q, self._kv_o = (kv.n_kv_heads, kv.d_qk), (kv.n_kv_heads, kv.d_v), (kv.n_heads, kv.d_qk), (kv.n_heads, kv.d_v)
+            self._kv_dev, self._kv_append, self._paged_attn = self.device.index or 0, lib().lsa_kv_append, lib().lsa_paged_attn
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         h = c_void_p()
@@ -339,44 +360,38 @@ class Context:
         """The arguments of a cache: pools as [rows, heads * dims] or [rows, heads, dims], scales as [rows, heads]."""
         if self.kv is None:
             raise LsaError(-1, where, "the context was made without kv parameters")
-        # (a look at a tensor's shape costs more than its number of elements)
-        rows = k_pool.numel() // self._kv_wk if k_pool.is_contiguous() else k_pool.shape[0]
+        dev, rows = self._kv_dev, k_pool.shape[0]
         n_pages, rest = divmod(rows, self._kv_page)
         if rest:
             raise LsaError(-1, where, f"a pool of {rows} rows is not a whole number of pages of {self._kv_page}")
-        sh = page_table.shape
-        if page_table.dtype is not torch.int32 or len(sh) != 2 or not (page_table.is_contiguous() or page_table.stride(1) == 1):
-            raise LsaError(-1, where, "page_table: int32 [batch, pages] with contiguous rows wanted")
-        batch, pitch = sh
-        if batch > 1 and not page_table.is_contiguous():
-            pitch = page_table.stride(0)
+        batch, pitch, pages = _kv_table(page_table, where, dev)
         cached = self._kv_codes.get(k_pool.dtype, torch.uint8) if self._kv_codes else self._kv_dtype
-        k, ld_k = _kv_rows(k_pool, self._kv_wk, cached, where, rows)
-        v, ld_v = _kv_rows(v_pool, self._kv_wv, cached, where, rows)
-        ks, vs = (None, None) if k_scale is None and v_scale is None else (_kv_flat(x, torch.float32, rows * self.kv.n_kv_heads, where) for x in (k_scale, v_scale))
-        return (k, ld_k, v, ld_v, ks, vs, n_pages, page_table.data_ptr(), pitch, _kv_flat(ctx_len, torch.int32, batch, where), batch)
+        k, ld_k = _kv_rows(k_pool, *self._kv_k, cached, where, rows, dev)
+        v, ld_v = _kv_rows(v_pool, *self._kv_v, cached, where, rows, dev)
+        ks, vs = (None, None) if k_scale is None and v_scale is None else (_kv_flat(x, torch.float32, rows * self._kv_k[0], where, dev) for x in (k_scale, v_scale))
+        return (k, ld_k, v, ld_v, ks, vs, n_pages, pages, pitch, _kv_flat(ctx_len, torch.int32, batch, where, dev), batch)
 
     def kv_append(self, k_new, v_new, k_pool, v_pool, page_table, ctx_len, ctx_len_out=None, tok_start=None, q=None, q_out=None,
                   cos_sin=None, k_scale=None, v_scale=None):
         """lsa_kv_append: new tokens [n_tok, heads, dims] into the cache, rotated; q (optional) rotated into q_out."""
         where = "lsa_kv_append"
         cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where)
-        batch, dtype, n_pos = cache[-1], self._kv_dtype, 0
-        n_tok = k_new.numel() // self._kv_wk if k_new.is_contiguous() else k_new.shape[0]
+        batch, dtype, n_pos, n_tok, dev = cache[-1], self._kv_dtype, 0, k_new.shape[0], self._kv_dev
         if cos_sin is not None:
             n_pos, width = cos_sin.shape if cos_sin.dim() == 2 else (0, -1)
             if width != self._kv_rope:
                 raise LsaError(-1, where, f"cos_sin: [positions, {self._kv_rope}] wanted, got {tuple(cos_sin.shape)}")
-        self._chk(lib().lsa_kv_append(
-            self.h, self._kv_ref, *_kv_rows(k_new, self._kv_wk, dtype, "k_new", n_tok), *_kv_rows(v_new, self._kv_wv, dtype, "v_new", n_tok),
-            *_kv_rows(q, self._kv_wq, dtype, "q", n_tok), *_kv_rows(q_out, self._kv_wq, dtype, "q_out", n_tok), n_tok,
-            _kv_flat(tok_start, torch.int32, batch + 1, "tok_start"), _kv_flat(cos_sin, torch.float32, n_pos * self._kv_rope, "cos_sin"), n_pos,
-            *cache, _kv_flat(ctx_len_out, torch.int32, batch, "ctx_len_out")), where)
+        self._chk(self._kv_append(
+            self.h, self._kv_ref, *_kv_rows(k_new, *self._kv_k, dtype, "k_new", n_tok, dev), *_kv_rows(v_new, *self._kv_v, dtype, "v_new", n_tok, dev),
+            *_kv_rows(q, *self._kv_q, dtype, "q", n_tok, dev), *_kv_rows(q_out, *self._kv_q, dtype, "q_out", n_tok, dev), n_tok,
+            _kv_flat(tok_start, torch.int32, batch + 1, "tok_start", dev), _kv_flat(cos_sin, torch.float32, n_pos * self._kv_rope, "cos_sin", dev), n_pos,
+            *cache, _kv_flat(ctx_len_out, torch.int32, batch, "ctx_len_out", dev)), where)
 
     def paged_attn(self, q, k_pool, v_pool, page_table, ctx_len, out, lse=None, k_scale=None, v_scale=None):
         """lsa_paged_attn: q [batch, heads, d_qk] over each sequence's cached tokens -> out [batch, heads, d_v], lse [batch, heads]."""
         where = "lsa_paged_attn"
         cache = self._kv_cache(k_pool, v_pool, k_scale, v_scale, page_table, ctx_len, where)
-        batch, dtype = cache[-1], self._kv_dtype
-        self._chk(lib().lsa_paged_attn(self.h, self._kv_ref, *_kv_rows(q, self._kv_wq, dtype, "q", batch), *cache,
-                                       *_kv_rows(out, self._kv_wo, dtype, "out", batch), _kv_flat(lse, torch.float32, batch * self.kv.n_heads, "lse")), where)
+        batch, dtype, dev = cache[-1], self._kv_dtype, self._kv_dev
+        self._chk(self._paged_attn(self.h, self._kv_ref, *_kv_rows(q, *self._kv_q, dtype, "q", batch, dev), *cache,
+                                   *_kv_rows(out, *self._kv_o, dtype, "out", batch, dev),
+                                   _kv_flat(lse, torch.float32, batch * self._kv_o[0], "lse", dev)), where)

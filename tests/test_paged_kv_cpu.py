@@ -157,14 +157,34 @@ def test_kinds_of_cache_and_their_pointers():
 def test_binding_refuses_tensors_of_another_form():
     """The binding's own checks, which need no library call."""
     x = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
-    assert binding._kv_rows(x, 1024, torch.bfloat16, "x", 6)[1] == 1024
+    assert binding._kv_rows(x, 8, 128, torch.bfloat16, "x", 6)[1] == 1024
+    assert binding._kv_rows(x.view(6, 1024), 8, 128, torch.bfloat16, "x", 6)[1] == 1024
     wide = torch.zeros(6, 20, 128, dtype=torch.bfloat16)
-    assert binding._kv_rows(wide[:, 4:12], 1024, torch.bfloat16, "x", 6)[1] == 2560
-    for bad in (x.float(), x[:5], x[:, :4], x[:, ::2], x[..., ::2], x.transpose(0, 1)):
+    assert binding._kv_rows(wide[:, 4:12], 8, 128, torch.bfloat16, "x", 6)[1] == 2560
+    for bad in (x.float(), x[:5], x[:, :4], x[:, ::2], x[..., ::2], x.transpose(0, 1), x.transpose(0, 1).contiguous(), x.transpose(1, 2).contiguous(), x.flatten(), x.view(3, 2, 8, 128)):
         with pytest.raises(binding.LsaError) as e:
-            binding._kv_rows(bad, 1024, torch.bfloat16, "x", 6)
+            binding._kv_rows(bad, 8, 128, torch.bfloat16, "x", 6)
         assert e.value.code == -1
     with pytest.raises(binding.LsaError):
         binding._kv_flat(torch.zeros(4, dtype=torch.int64), torch.int32, 4, "n")
     with pytest.raises(binding.LsaError):
         binding._kv_flat(torch.zeros(4, dtype=torch.int32), torch.int32, 5, "n")
+    for call in (lambda: binding._kv_rows(x, 8, 128, torch.bfloat16, "x", 6, 0), lambda: binding._kv_flat(torch.zeros(4), torch.float32, 4, "x", 0),
+                 lambda: binding._kv_table(torch.zeros(2, 3, dtype=torch.int32), "x", 0)):
+        with pytest.raises(binding.LsaError) as e:      # host memory where the device's is wanted
+            call()
+        assert e.value.code == -1
+
+
+def test_binding_looks_at_page_tables():
+    """The kernels may follow a row of the table up to its pitch."""
+    big = torch.zeros(4, 10, dtype=torch.int32)
+    assert binding._kv_table(big, "t")[:2] == (4, 10)
+    assert binding._kv_table(big[:, :6], "t")[:2] == (4, 10)        # the first columns: every row's pitch is there
+    assert binding._kv_table(big[:3, 4:8], "t")[:2] == (3, 10)      # (another row follows)
+    assert binding._kv_table(big[1:2, 4:8], "t")[:2] == (1, 4)
+    assert binding._kv_table(big[:0], "t")[0] == 0
+    for bad in (big[:, 4:], big.t(), big[:, ::2], big[:1, ::2], big[0], big.long(), big[:1].expand(4, 10)):
+        with pytest.raises(binding.LsaError) as e:
+            binding._kv_table(bad, "t")
+        assert e.value.code == -1
