@@ -28,6 +28,9 @@ using paged::exp2_fast;
 constexpr int kWarps = 8, kThreads = 32 * (kWarps + 1);   // and the one that copies
 constexpr int kRing = 6;
 
+template <int V>
+struct IntC { static constexpr int value = V; };
+
 // kTiles: groups of eight query heads per KV head (1 or 2).
 template <int D, bool kE4M3, int kTiles>
 struct Shape {
@@ -120,6 +123,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
     const int beyond = static_cast<int>(static_cast<int64_t>(max(p.n_pages, 1)) << p.page_shift);   // the first row past the pool: rows of zeros
     const int box_bytes = (S::kBytes >> shift) << box_shift;   // (a tile's bytes over its keys, times a box's)
     const int n_boxes = 1 << (shift - box_shift);
+    // scales of consecutive rows follow one another where a block has all heads: 16 bytes a copy; else 2^copy_shift heads of a row
+    // (155 sequences of 1640 tokens, one KV head, pages of 16, by rows and boxes: 41.4 us; so: 22.3)
+    const int copy_shift = blocks == 1 ? 2 : min(heads_shift, 2);
     // a lane's box of the tile at the cursor: its cache row; past the pool if its page is not one, -1 if nobody sees its keys
     auto row_of = [&]() -> int {
       if (cur.left <= 0 || lane >= n_boxes) return -1;
@@ -154,19 +160,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if constexpr (kE4M3) {
           const float* src = kv == 0 ? p.k_scale : p.v_scale;
           const uint32_t dst = smem_u32(scales) + slot * S::kScales;
-          for (int j = 0; j < n_boxes; ++j) {   // rows of 4, 8, 16 or 32 bytes, a lane each
-            const int r0 = __shfl_sync(0xffffffffu, this_row, j);
-            if (r0 < 0) continue;
-            for (int i = lane; i < 1 << box_shift; i += 32) {
-              const int r = (j << box_shift) + i;
-              const float* s = src + (r0 < beyond ? static_cast<int64_t>(r0 + i) * p.G + head0 : 0);
+          auto fetch = [&](auto floats_c) {   // so many floats a copy
+            constexpr int kFloats = decltype(floats_c)::value;
+#pragma unroll
+            for (int i = 0; i < kWarps * R / kFloats / 32; ++i) {
+              const int f = (32 * i + lane) * kFloats, r = f >> heads_shift;   // the copy's first float in the slot, its row
+              const int r0 = __shfl_sync(0xffffffffu, this_row, r >> box_shift);
               const bool there = r0 < beyond;
-              if (heads_shift == 0) cp_async_ca<4>(dst + r * 4, s, there ? 4 : 0);
-              else if (heads_shift == 1) cp_async_ca<8>(dst + r * 8, s, there ? 8 : 0);
-              else
-                for (int h = 0; h < 1 << (heads_shift - 2); ++h) cp_async_ca<16>(dst + (r << (heads_shift + 2)) + 16 * h, s + 4 * h, there ? 16 : 0);
+              const float* s = src + (there ? static_cast<int64_t>(r0 + (r & ((1 << box_shift) - 1))) * p.G + head0 + (f & ((1 << heads_shift) - 1)) : 0);
+              if (r0 >= 0) cp_async_ca<4 * kFloats>(dst + 4 * f, s, there ? 4 * kFloats : 0);
             }
-          }
+          };
+          if (copy_shift == 2) fetch(IntC<4>{});
+          else if (copy_shift == 1) fetch(IntC<2>{});
+          else fetch(IntC<1>{});
           cp_async_arrive(bar);
         }
         __syncwarp();
@@ -593,8 +600,6 @@ __device__ __forceinline__ float lanes_sum(float x, int from) {
   for (int o = from; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
-template <int V>
-struct IntC { static constexpr int value = V; };
 __device__ __forceinline__ void add(float4& x, float w, const float4& y) { x.x += w * y.x; x.y += w * y.y; x.z += w * y.z; x.w += w * y.w; }
 
 template <typename T>
