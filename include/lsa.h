@@ -434,7 +434,8 @@ LSA_API int lsa_kv_append(lsa_ctx* ctx, const lsa_kv_params* p, const void* k_ne
  *   lse        optional fp32 [batch, n_heads]
  *   k_pool ... page_table as in lsa_kv_append; ctx_len int32 [batch]: lengths with the new token
  * The cached tokens of all sequences are dealt evenly to the SMs, and parts of a sequence are joined by their log-sum-exps (in
- * a fixed order: the same call gives the same bits).  A sequence's rounding depends on the batch that it is dealt with.
+ * a fixed order: the same call gives the same bits).  A sequence's rounding depends on the batch that it is dealt with.  The parts
+ * lie in the context's workspace: calls of one context, and graphs captured from them, must not run at the same time.
  * A length outside [0, page_table_stride * kv_page] (it is clamped to that range) or a page number outside [0, n_pages) (its tokens count
  * as zero rows) is reported as LSA_ERR_INDEX by lsa_status; other sequences are not affected. */
 LSA_API int lsa_paged_attn(lsa_ctx* ctx, const lsa_kv_params* p, const void* q, int64_t ld_q, const void* k_pool, int64_t ld_k,

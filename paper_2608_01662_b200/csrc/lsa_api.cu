@@ -849,7 +849,7 @@ static int check_kv_params(const lsa_kv_params* p) {
     if (flag != 0 && flag != 1) return LSA_ERR_ARG;
   if (p->n_heads <= 0 || p->n_kv_heads <= 0 || p->n_heads % p->n_kv_heads != 0) return LSA_ERR_ARG;
   if (p->k_sink < 0 || p->k_swa < 0 || p->d_rope < 0 || p->rope_at < 0) return LSA_ERR_ARG;
-  if (!(p->sm_scale > 0.f) || !(p->sm_scale < 3e38f)) return LSA_ERR_ARG;
+  if (!(p->sm_scale > 0.f) || !(p->sm_scale < 2e38f)) return LSA_ERR_ARG;   // (times log2(e) it is still a number)
   if (p->latent) {
     if (p->n_kv_heads != 1 || p->n_heads > 64 || p->d_qk != 576 || p->d_v != 512 || p->cache_e4m3) return LSA_ERR_SHAPE;
     if (p->kv_page != 64 && p->kv_page != 128 && p->kv_page != 256) return LSA_ERR_SHAPE;

@@ -76,7 +76,7 @@ def test_parameters_struct():
     (dict(n_heads=65), -2), (dict(n_heads=0), -1), (dict(d_qk=512), -2), (dict(d_v=576), -2), (dict(e4m3=True), -2),
     (dict(kv_page=32), -2), (dict(kv_page=512), -2), (dict(n_kv_heads=2), -2), (dict(d_rope=8), -2), (dict(d_rope=64, rope_at=520), -2),
     (dict(d_rope=64, rope_at=528), -2), (dict(d_rope=-16), -1), (dict(sm_scale=0.0), -1), (dict(sm_scale=-1.0), -1), (dict(sm_scale=math.nan), -1),
-    (dict(sm_scale=math.inf), -1), (dict(sink=-1), -1), (dict(window=-5), -1)])
+    (dict(sm_scale=math.inf), -1), (dict(sm_scale=2.5e38), -1), (dict(sink=-1), -1), (dict(window=-5), -1)])
 def test_latent_parameters_refused(change, code):
     with pytest.raises(binding.LsaError) as e:
         binding.kv_workspace_bytes(binding.make_kv_params(**{**MLA, **change}))
