@@ -972,7 +972,6 @@ int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld
   a.sink = p->k_sink; a.window = p->k_swa; a.page_shift = log2_of(p->kv_page); a.batch = batch;
   a.max_len = static_cast<int>(page_table_stride * p->kv_page); a.n_pages = static_cast<int>(n_pages);
   a.units = c->sm_count < lsa::kMaxPagedUnits ? c->sm_count : lsa::kMaxPagedUnits;
-  a.min_tiles = p->latent ? 1 : 2;
   a.pt_stride = page_table_stride; a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out;
   a.scale2 = p->sm_scale * 1.4426950408889634f;
   a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;
