@@ -972,6 +972,10 @@ int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld
   a.sink = p->k_sink; a.window = p->k_swa; a.page_shift = log2_of(p->kv_page); a.batch = batch;
   a.max_len = static_cast<int>(page_table_stride * p->kv_page); a.n_pages = static_cast<int>(n_pages);
   a.units = c->sm_count < lsa::kMaxPagedUnits ? c->sm_count : lsa::kMaxPagedUnits;
+  // A part of latent rows is 128 KB to write and to join, and a tile more costs less (up to 0, 2, 3, 5 tiles: 64 sequences of 300 tokens
+  // 22.5, 15.6, 15.5, 15.6 us; 256 of 400 52.5, 46.5, 40.4, 40.4; 100 of 374 to 2906 50.7, 47.7, 47.7, 48.5).  Parts of separate keys and
+  // values are small (0, 1, 2, 4: 155 of 374 to 2906, one KV head 24.0, 26.5, 30.5, 33.9; 8 of 1000, 8 KV heads 14.0, 13.9, 12.0, 12.6).
+  a.near = p->latent ? 3 : 0;
   a.pt_stride = page_table_stride; a.ld_q = ld_q; a.ld_k = ld_k; a.ld_v = ld_v; a.ld_out = ld_out;
   a.scale2 = p->sm_scale * 1.4426950408889634f;
   a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;

@@ -248,6 +248,7 @@ struct PagedAttnArgs {
   int max_len;                // tokens that a row of the page table covers
   int n_pages;
   int units;                  // blocks that the list of tiles is dealt to
+  int near;                   // tiles that a cut of the list is moved by at most to an end of a sequence
   int64_t pt_stride, ld_q, ld_k, ld_v, ld_out;
   float scale2;               // sm_scale * log2(e)
   const void *q, *k_pool, *v_pool;

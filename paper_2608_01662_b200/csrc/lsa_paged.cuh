@@ -74,13 +74,14 @@ __device__ __forceinline__ SeqTiles seq_tiles(const PagedAttnArgs& a, int b, int
 struct Cursor {
   int b, block, tile;   // sequence, block of KV heads, tile
   int left;             // entries of the unit from here on
-  int per;              // entries of every unit but the last
+  int per, near;        // see first_entry
   SeqTiles st;
 };
-// By a whole warp: unit u's first entry.  Each lane counts a run of consecutive sequences.  (The list has fewer than 2^31
-// entries: the host sees to that.)
+// By a whole warp: unit u's first entry.  The list is cut every `per` entries, and a cut no more than `near` from an end of its (sequence,
+// block) is moved there: a tile more costs a unit less than a part that has to be written and joined.
+// (The list has fewer than 2^31 entries: the host sees to that.)
 __device__ __forceinline__ Cursor first_entry(const PagedAttnArgs& a, int unit, int shift, int blocks, int lane) {
-  const int run = (a.batch + 31) / 32;
+  const int run = (a.batch + 31) / 32;   // each lane counts a run of consecutive sequences
   int mine = 0, n = 0;
   for (int i = 0; i < run; ++i) {
     const int b = lane * run + i;
@@ -101,26 +102,43 @@ __device__ __forceinline__ Cursor first_entry(const PagedAttnArgs& a, int unit, 
   // (down to one tile each, though every part has to be joined: at least two took 11.8 us instead of 11.3 for one latent sequence of 300
   // tokens, 17.2 instead of 13.0 for four of 777, and 9.5 instead of 9.3 for one of 2000 with 8 KV heads)
   c.per = (total - 1) / a.units + 1;
+  c.near = min(a.near, c.per - 1);
   const int64_t t0 = static_cast<int64_t>(unit) * c.per;
   if (t0 >= total) return c;
-  c.left = min(c.per, total - static_cast<int>(t0));
-  const int owner = __ffs(__ballot_sync(0xffffffffu, upto > t0)) - 1;
-  int off = static_cast<int>(t0) - __shfl_sync(0xffffffffu, upto - mine, owner);
-  c.b = owner * run;
-  if (run == 1) {   // (the owner has the length: a load less on the way to the first tile)
-    c.st = tiles_of(a, __shfl_sync(0xffffffffu, n, owner), shift);
-  } else {
-    c.st = seq_tiles(a, c.b, shift);
-    while (c.st.count * blocks <= off) {
-      off -= c.st.count * blocks;
-      c.st = seq_tiles(a, ++c.b, shift);
+  auto locate = [&](int at) {   // entry `at`
+    const int owner = __ffs(__ballot_sync(0xffffffffu, upto > at)) - 1;
+    int off = at - __shfl_sync(0xffffffffu, upto - mine, owner);
+    c.b = owner * run;
+    c.block = 0;
+    if (run == 1) {   // (the owner has the length: a load less on the way to the first tile)
+      c.st = tiles_of(a, __shfl_sync(0xffffffffu, n, owner), shift);
+    } else {
+      c.st = seq_tiles(a, c.b, shift);
+      while (c.st.count * blocks <= off) {
+        off -= c.st.count * blocks;
+        c.st = seq_tiles(a, ++c.b, shift);
+      }
     }
+    while (off >= c.st.count) {   // (`blocks` is small)
+      off -= c.st.count;
+      ++c.block;
+    }
+    c.tile = off;
+  };
+  auto cut = [&](int at) -> int {   // where the cut before entry `at` comes to lie
+    locate(at);
+    const int rest = c.st.count - c.tile;
+    return min(c.tile, rest) > c.near ? at : c.tile <= rest ? at - c.tile : at + rest;
+  };
+  const int first = static_cast<int>(t0), next = first + min(c.per, total - first);
+  if (c.near == 0) {
+    c.left = next - first;
+    locate(first);
+    return c;
   }
-  while (off >= c.st.count) {   // (`blocks` is small)
-    off -= c.st.count;
-    ++c.block;
-  }
-  c.tile = off;
+  const int end = next < total ? cut(next) : total, start = cut(first);
+  c.left = end - start;
+  if (c.left > 0 && start != first) locate(start);
   return c;
 }
 // The next entry; true: it belongs to another (sequence, block).
@@ -144,7 +162,7 @@ __device__ __forceinline__ bool advance(const PagedAttnArgs& a, Cursor& c, int s
 __device__ __forceinline__ void say_parts(const PagedAttnArgs& a, int unit, const Cursor& last, bool begins_here, bool first) {
   const int rest = last.st.count - (last.tile + 1);
   const bool goes_on = begins_here && rest > 0;
-  a.parts[unit] = make_int4(goes_on ? 1 + (rest + last.per - 1) / last.per : 0, last.b, last.block, 2 * unit + (first ? 0 : 1));
+  a.parts[unit] = make_int4(goes_on ? 1 + (rest - last.near + last.per - 1) / last.per : 0, last.b, last.block, 2 * unit + (first ? 0 : 1));
 }
 
 // ---- the kernels that join parts: what a block has to do.
