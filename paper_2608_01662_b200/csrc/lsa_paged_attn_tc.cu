@@ -492,7 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1) paged_latent_kernel(const __grid_
             for (int i = 0; i < 4; ++i) w[i] = pack2<kF16>(__uint_as_float(o[8 * j + 2 * i]) * inv, __uint_as_float(o[8 * j + 2 * i + 1]) * inv);
             *reinterpret_cast<uint4*>(stage + head_o * 1024 + ((((dim0 + c) / 8 + j) ^ (head_o & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
           }
-        } else {   // a part: four dims of each head, the lanes' heads side by side (a row of its own per lane took 10 thousand cycles to store)
+        } else if (head_o < p.H) {   // a part: four dims of each head, the lanes' heads side by side (a row of its own per lane took 10 thousand cycles to store)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
             *reinterpret_cast<float4*>(part + (c + 4 * j) * kHeads) =
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) paged_latent_join_kernel(Page
       float w[kParts], m = -INFINITY, den = 0.f;
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
-        w[i] = i < n ? __ldcg(a.part_lse + slot(i) * kHeads + head) : -INFINITY;
+        w[i] = i < n && head < a.H ? __ldcg(a.part_lse + slot(i) * kHeads + head) : -INFINITY;
         m = fmaxf(m, w[i]);
       }
       const float ref = m > -INFINITY ? m : 0.f;
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) paged_latent_join_kernel(Page
       float4 x[kMine / 4] = {};
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
-        if (i < n) {
+        if (i < n && head < a.H) {
           const float* src = a.part_out + (slot(i) * kDV + round * kDims + way * kMine) * kHeads + 4 * head;
           const float wi = w[i] * inv;
 #pragma unroll
@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(kJoinThreads, 2) paged_latent_join_kernel(Page
           const int i = i0 + k * kWays;
           w[k] = -INFINITY;
           y[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (i < n) {
+          if (i < n && head < a.H) {
             w[k] = __ldcg(a.part_lse + slot(i) * kHeads + head);
             y[k] = __ldcg(reinterpret_cast<const float4*>(src + slot(i) * kDV * kHeads));
           }
