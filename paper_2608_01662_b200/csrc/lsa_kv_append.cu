@@ -5,7 +5,11 @@
 // eight pairs (x cos - y sin, y cos + x sin), so the angles' cosines and sines are fetched once per thread, not once per head; a
 // row's threads are consecutive lanes, so the largest element of an e4m3 row is a few shuffles.
 //
-// Bound: HBM for prompts (read and write once), a launch and the chain length -> page -> row for decode steps.
+// Bound: HBM for prompts (read and write once: 17.5 thousand tokens, 32 query and 8 KV heads of 128, 70 us, 0.94 of a copy's rate; 9871
+// tokens, 64 query heads, e4m3 caches 69 us, 0.86), a launch and the chain length -> page -> row for decode steps (4.7 us).  Rows are on their way before the
+// token's place is known, and no load stands behind a branch (with branches around the loads: 90 us instead of 69).
+#include <algorithm>
+
 #include "lsa_paged.cuh"
 
 namespace lsa {
@@ -73,17 +77,25 @@ __device__ __forceinline__ int32_t new_length(const KvAppendArgs& a, int i) {
   return a.ctx_len[i] + max(t1 - t0, 0);
 }
 
-constexpr int kQAtOnce = 4, kKvAtOnce = 2;   // rows that a thread has on their way
-// Threads of a block: few tokens get a block that has all rows of 64 heads on their way at once; of many tokens several share an
-// SM, and a thread has enough rows to be worth the look-up of the token's place.
+// Threads of a block.  A token's rows are shared by 64 threads (288 for the latent rows of 36 places), so that many tokens are on an SM
+// at a time; where there is at most one token an SM, and its rows are more than those threads have on their way, by 512 (576).  96
+// query and 8 KV heads of 128: 148 tokens 3.9 us by 512 threads, 5.2 by 64; 250 tokens 6.7, 5.2; 32 query heads: 148 tokens 3.3, 2.7.
 template <int D>
 constexpr int kFewTokens = D == 576 ? 576 : 512;
 template <int D>
 constexpr int kManyTokens = D == 576 ? 288 : 64;
+// Query rows that a thread has on their way at a time: four, or two where the block's threads then have all of them, and more blocks
+// fit an SM (5000 tokens of latent rows: 16 heads 65 us by four, 51 by two; 64 heads 134, 139).  A block of 288 threads is nine warps, so
+// that of two one SM partition has five: they fit with 96 registers each, which is what a bound of two blocks of ten warps gives.
+template <int kThreads>
+constexpr int kBound = kThreads == 288 ? 320 : kThreads;
+template <int kThreads, int kQAtOnce>
+constexpr int kBlocks = kThreads != 288 ? 1 : kQAtOnce == 2 ? 3 : 2;
 
 // D: dims of a query or key head (and of a value head, if there are any).  kThreads: a multiple of 32 and of D / 16.
-template <typename T, int D, bool kE4M3, int kThreads>
-__global__ void __launch_bounds__(kThreads) kv_append_kernel(KvAppendArgs a) {
+template <typename T, int D, bool kE4M3, int kThreads, int kQAtOnce>
+__global__ void __launch_bounds__(kBound<kThreads>, kBlocks<kThreads, kQAtOnce>) kv_append_kernel(KvAppendArgs a) {
+  constexpr int kKvAtOnce = D == 576 ? 1 : 2;   // (a token has one latent row)
   constexpr int kPlaces = D / 16, kRows = kThreads / kPlaces;   // threads of a row, rows of a block at a time
   static_assert(kThreads % 32 == 0 && kThreads % kPlaces == 0, "whole rows");
   const int tid = threadIdx.x;
@@ -282,8 +294,11 @@ __global__ void kv_lengths_kernel(KvAppendArgs a) {
 template <typename T, int D, bool kE4M3>
 cudaError_t launch_t(const KvAppendArgs& a, cudaStream_t st) {
   const dim3 grid(static_cast<unsigned>(a.n_tok));
-  if (a.n_tok <= 2 * a.sm_count) return launch_pdl(kv_append_kernel<T, D, kE4M3, kFewTokens<D>>, grid, dim3(kFewTokens<D>), 0, st, a);
-  return launch_pdl(kv_append_kernel<T, D, kE4M3, kManyTokens<D>>, grid, dim3(kManyTokens<D>), 0, st, a);
+  constexpr int kFew = kFewTokens<D>, kMany = kManyTokens<D>, kRows = kMany / (D / 16);   // rows of the smaller block at a time
+  const int rows = std::max(a.q != nullptr ? a.H : 0, a.latent ? 1 : 2 * a.G);
+  if (a.n_tok <= a.sm_count && rows > 4 * kRows) return launch_pdl(kv_append_kernel<T, D, kE4M3, kFew, 4>, grid, dim3(kFew), 0, st, a);
+  if (D == 576 && rows <= 2 * kRows) return launch_pdl(kv_append_kernel<T, D, kE4M3, kMany, 2>, grid, dim3(kMany), 0, st, a);
+  return launch_pdl(kv_append_kernel<T, D, kE4M3, kMany, 4>, grid, dim3(kMany), 0, st, a);
 }
 template <typename T>
 cudaError_t launch_d(const KvAppendArgs& a, cudaStream_t st) {

@@ -3,18 +3,26 @@
 //
 // A token's 1152 bytes meet 64 heads: 121 flop per byte, so HBM is the bound only as long as the products run on tcgen05 and
 // the softmax stays beside them.  The 64 heads are the M = 64 rows of every MMA (rows of absent heads are zero).  A unit of the
-// grid works through its share of the list of 64-token tiles (lsa_paged.cuh), one (sequence) after another:
+// grid works through its share of the list of 64-token tiles (lsa_paged.cuh), one sequence after another:
 //
 //   warp 8      copies: a tile lies inside one cache page, so each half of it is one TMA box (nine column blocks of 32 rows x 128
-//               bytes, 128B-swizzled), into a ring of six such slots.  Every slot is 36.9 KB.
-//   warps 9, 10 S = Q K^T, a half of the tile each, M64 N32 K16, Q in tensor memory (its last 64 dims in shared memory), as two accumulation chains
-//               in the two halves of the lanes (an M = 64 accumulator uses 16 lanes of each 32); two S buffers.
-//   warps 0-7   softmax, four warps for each half of a tile's keys: the two partial sums are added, P = 2^(score - max) with the running
-//               maximum as it is, fp32 row sums, P in 16 bits into the slot's last column block, which only Q K^T reads; one vote
-//               says whether the maximum was good enough for every row (O is rescaled, and P worked out again, only when a row
-//               grows by more than 2^8).  At a sequence's end they fetch the next Q and write O.  Rows of a tile that nobody
-//               sees are zeroed there before they become values: 0 x NaN is NaN.
+//               bytes, 128B-swizzled), into a ring of three tiles, two slots of 36.9 KB each.  A sequence's Q (32 heads a slot)
+//               goes through the ring too, ahead of its first tile.
+//   warps 9, 10 S = Q K^T, a half of each tile's keys per warp, M64 N32 K16.  Q is in tensor memory (its last 64 dims in shared
+//               memory), and S has two accumulation chains in the two halves of the lanes (an M = 64 accumulator uses 16 lanes of
+//               each 32); two S buffers.
+//   warps 0-7   softmax, four warps for each half of a tile's keys: the two partial sums are added, P = 2^(score - reference) with
+//               the reference as it is, fp32 row sums, P in 16 bits into the slot's last column block, which only Q K^T reads; one
+//               vote says whether the reference was good enough for every row (O is rescaled, and P worked out again, only when a
+//               row's maximum has grown by more than 2^8).  At a sequence's end they move the next Q and write O.  Rows of a tile
+//               that nobody sees are zeroed there before they become values: 0 x NaN is NaN.
 //   warp 11     O += P V, tcgen05.mma.ws M64 N256 K16; V is the tile read MN-major, so a row is fetched once.
+//
+// Measured: one sequence of 524 thousand tokens 120 us (5.0 TB/s, 0.77 of a copy's rate), 64 sequences with 3.5 million 690-820 us (the
+// GPU is then at its power limit, 990 W, at 1.0 to 1.4 of its 1.97 GHz: a tile takes 2160 or 2500 cycles and the same time), one of a
+// few hundred tokens 11 us, of which 4 pass before the first tile is there and 3 to 4 in the kernel that joins.  Tiles of 32 tokens took
+// 1475 cycles each: the softmax's chain from one to the next, not its work.  One issuing thread for both halves of Q K^T made the
+// second half's softmax wait (130 us instead of 120).
 //
 // Tensor memory columns:   0-255  O: value dims 0-255 in columns 0-127, 256-511 in 128-255; lanes 0-63 hold the first 128
 //                                 dims of each, lanes 64-127 the second, lane l (mod 64) = head l
