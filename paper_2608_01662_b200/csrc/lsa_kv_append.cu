@@ -6,8 +6,8 @@
 // row's threads are consecutive lanes, so the largest element of an e4m3 row is a few shuffles.
 //
 // Bound: HBM for prompts (read and write once: 17.5 thousand tokens, 32 query and 8 KV heads of 128, 70 us, 0.94 of a copy's rate; 9871
-// tokens, 64 query heads, e4m3 caches 69 us, 0.86), a launch and the chain length -> page -> row for decode steps (4.7 us).  Rows are on their way before the
-// token's place is known, and no load stands behind a branch (with branches around the loads: 90 us instead of 69).
+// tokens, 64 query heads, e4m3 caches 68 us, 0.87), a launch and the chain length -> page -> row for decode steps (3 to 5 us).  Rows are
+// on their way before the token's place is known, and no load stands behind a branch (with branches around the loads: 90 us, not 69).
 #include <algorithm>
 
 #include "lsa_paged.cuh"

@@ -1,8 +1,9 @@
 // Paged key-value caches: what lsa_kv_append and lsa_paged_attn share.
 //
 // lsa_paged_attn deals the key tiles of all sequences out evenly: they form one list, ordered by (sequence, block of KV heads,
-// position), and unit u of the grid takes entries [u * per, (u + 1) * per).  Lengths differ by orders of magnitude between sequences,
-// and a grid by sequence would wait for the longest.  Every unit, and the kernel that joins the parts, derives the same list from ctx_len.
+// position), and unit u of the grid (a block per SM) takes entries [u * per, (u + 1) * per).  Lengths differ by orders of magnitude
+// between sequences, and a grid by sequence would wait for the longest.  Every unit derives the same list from ctx_len and leaves word of
+// what there is to join, so the host needs no lengths and a captured call stays right as they grow.
 #pragma once
 
 #include "lsa_common.cuh"
@@ -166,7 +167,7 @@ __device__ __forceinline__ void say_parts(const PagedAttnArgs& a, int unit, cons
 }
 
 // ---- the kernels that join parts: what a block has to do.
-// The units' words about their parts give each owner (a unit that holds a beginning) a number of rounds; round `it` of all of them is
+// The units' words about their parts (148 numbers, whatever the batch) give each owner (a unit that holds a beginning) a number of rounds; round `it` of all of them is
 // looked up by the threads together.
 constexpr int kJoinThreads = 256;
 struct JoinList {

@@ -588,7 +588,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 // ---- parts of a sequence that several units worked on -------------------------------------------------
 // Weights 2^(lse_i - max) / sum over the parts, a fixed order of addition.  A warp joins a row of few parts, or 32 dims of a row of some;
 // the warps of a block share 32 dims of a row of many (a long sequence on its own is a part in every unit, and all SMs have to
-// fetch them together).
+// fetch them together).  Attention with it, 32 query and 8 KV heads: 64 sequences of 600 tokens, two or three parts each, 35.4 us, as some
+// parts 38.7; 16 of 1500, ten parts, 26.7, as many 35.5; one of 16000, 148 parts, 19.2.
 constexpr int kJoinWarps = 8, kFewParts = 8, kSomeParts = 32, kManyDims = 32;
 template <typename T>
 __device__ __forceinline__ void store4(T* out, const float4& x) {

@@ -21,8 +21,8 @@
 // Measured: one sequence of 524 thousand tokens 120 us (5.0 TB/s, 0.77 of a copy's rate), 64 sequences with 3.5 million 690-820 us (the
 // GPU is then at its power limit, 990 W, at 1.0 to 1.4 of its 1.97 GHz: a tile takes 2160 or 2500 cycles and the same time), one of a
 // few hundred tokens 11 us, of which 4 pass before the first tile is there and 3 to 4 in the kernel that joins.  Tiles of 32 tokens took
-// 1475 cycles each: the softmax's chain from one to the next, not its work.  One issuing thread for both halves of Q K^T made the
-// second half's softmax wait (130 us instead of 120).
+// 1475 cycles each: the softmax's chain from one to the next, not its work.  One issuing thread for both halves of Q K^T stalls for
+// some 400 cycles behind each commit (the first sequence 122.5 us instead of 118.5, the 64 733 instead of 690).
 //
 // Tensor memory columns:   0-255  O: value dims 0-255 in columns 0-127, 256-511 in 128-255; lanes 0-63 hold the first 128
 //                                 dims of each, lanes 64-127 the second, lane l (mod 64) = head l
