@@ -266,3 +266,53 @@ def test_many_small_weights(cuda_device):
     ctx, out, lse = pu.attend(c)
     assert ctx.status() == 0
     pu.check_attend(c, out, lse, sequences=[0, 7, 39])
+
+
+@pytest.mark.parametrize("shape", [(2, 1, 128, 128), (6, 2, 64, 64), (6, 3, 64, 64), (12, 6, 128, 128), (12, 12, 64, 64), (32, 16, 128, 128)])
+@pytest.mark.parametrize("page", [16, 64, 256])
+def test_scales_of_e4m3_caches(cuda_device, shape, page):
+    """Scales come in copies of one, two or four heads of a row, or of whole rows, out of boxes of a page."""
+    c = pu.Cache([1, 15, 33, 255, 256, 257, 700], shape, page, "bf16", True, cuda_device, seed=22, poison=True)
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_bad_page_counts_as_zero_rows(cuda_device, e4m3):
+    c = pu.Cache([200, 333], (4, 1, 64, 64), 16, "bf16", e4m3, cuda_device, seed=23)
+    for page in (-1, c.n_pages, 2 ** 31 - 1):
+        c.page_table[1, 3] = page
+        ctx, out, lse = pu.attend(c)
+        assert ctx.status() == -7
+        zero = int(c.table[1, 3])
+        keep = c.table.copy()
+        rows = slice(zero * 16, zero * 16 + 16)
+        old = [None if t is None else t[rows].clone() for t in (c.k, c.v)]
+        c.k[rows] = 0
+        c.v[rows] = 0
+        pu.check_attend(c, out, lse)
+        c.k[rows], c.v[rows] = old
+        assert np.array_equal(keep, c.table)
+
+
+def test_two_contexts_on_two_streams(cuda_device):
+    """Calls that run at the same time, each with its own workspace."""
+    cs = [pu.Cache([2000, 3, 700], (16, 2, 128, 128), 64, "bf16", False, cuda_device, seed=24), pu.Cache([300, 5000], (64, 1, 576, 512), 64, "bf16", False, cuda_device, seed=25)]
+    streams = [torch.cuda.Stream(cuda_device) for _ in cs]
+    calls = []
+    torch.cuda.synchronize()
+    for c, st in zip(cs, streams):
+        with torch.cuda.stream(st):
+            ctx = binding.Context(None, 0, 0, len(c.lengths), device=cuda_device, stream=st, kv=c.params())
+            calls.append(pu.attend(c, ctx))
+    torch.cuda.synchronize()
+    first = [(out.clone(), lse.clone()) for _, out, lse in calls]
+    for _ in range(20):
+        for c, st, (ctx, out, lse) in zip(cs, streams, calls):
+            with torch.cuda.stream(st):
+                pu.attend(c, ctx, out, lse)
+    torch.cuda.synchronize()
+    for c, (ctx, out, lse), (out1, lse1) in zip(cs, calls, first):
+        assert ctx.status() == 0 and torch.equal(out, out1) and torch.equal(lse, lse1)
+        pu.check_attend(c, out, lse)

@@ -203,3 +203,12 @@ def test_many_small_weights(cuda_device):
     ctx, out, lse = pu.attend(c)
     assert ctx.status() == 0
     pu.check_attend(c, out, lse, sequences=[0, 7, 39])
+
+
+@pytest.mark.parametrize("lengths", [[300] * 64, [400] * 150, [64 * k for k in range(1, 40)], [1000, 0, 1] * 25, [63, 65, 64 * 8, 64 * 7 + 1] * 20])
+def test_cuts_near_the_ends_of_sequences(cuda_device, lengths):
+    """Lists whose cuts fall near sequences' ends and are moved there, beside others that are not."""
+    c = pu.Cache(lengths, (3, 1, 576, 512), 64, "bf16", False, cuda_device, seed=26, poison=True)
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse)
