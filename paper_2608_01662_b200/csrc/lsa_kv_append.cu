@@ -5,7 +5,7 @@
 // eight pairs (x cos - y sin, y cos + x sin), so the angles' cosines and sines are fetched once per thread, not once per head; a
 // row's threads are consecutive lanes, so the largest element of an e4m3 row is a few shuffles.
 //
-// Bound: HBM for prompts (read and write once: 17.5 thousand tokens, 32 query and 8 KV heads of 128, 70 us, 0.94 of a copy's rate; 9871
+// Bound: HBM for prompts (read and write once: 17 thousand tokens, 32 query and 8 KV heads of 128, 70 us, 0.94 of a copy's rate; 9871
 // tokens, 64 query heads, e4m3 caches 68 us, 0.87), a launch and the chain length -> page -> row for decode steps (3 to 5 us).  Rows are
 // on their way before the token's place is known, and no load stands behind a branch (with branches around the loads: 90 us, not 69).
 #include <algorithm>
