@@ -17,10 +17,11 @@
 // that: 91 us).  Short sequences take 8 to 10 us: 4 until the first tile is there, the rest its work and the kernel that joins.
 //
 // e4m3 caches: a code is exact in fp16, and so is a query scaled by a power of two of its own head, so the scores' products
-// are fp16 MMAs of codes and the scale of a key is applied to the score.  A value's scale is applied to its weight before that is
-// rounded to bf16 (which has the range for any scale); the codes become bf16, exactly.  Those conversions are half of the
-// instructions (issue slots 51 % busy, against 20 % for 16-bit caches) and keep these
-// caches at 0.82 of a copy's rate (32 sequences of up to 32 thousand tokens, 8 KV heads, 774 MB in 141 to 146 us).
+// are fp16 MMAs of codes and the scale of a key is applied to the score.  A value's scale is applied to its weight; the product, times a
+// power of two of its head's own that follows the largest of them, is rounded to fp16: scales of any size, and what lies 2^-21 below
+// the largest product still has all its bits.  (With weights times scales in bf16 and codes turned into bf16 139 to 146 us instead
+// of 137, and a third more error.)  The conversions of codes keep these caches at 0.86 of a copy's rate (32 sequences of up to 32
+// thousand tokens, 64 query and 8 KV heads, 774 MB in 137 us).
 #include "lsa_paged.cuh"
 #include "lsa_tc.cuh"
 
@@ -92,8 +93,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, PagedAttnArgs p, int heads_shift) {
   using S = Shape<D, kE4M3, kTiles>;
   constexpr bool kF16 = !__is_same(T, __nv_bfloat16);
-  constexpr bool kQkF16 = kF16 || kE4M3, kPvF16 = kF16 && !kE4M3;
-  constexpr float kGap = paged::kRescaleGap + paged::kLift<kPvF16>;
+  constexpr bool k16 = kF16 || kE4M3;   // both products of fp16 numbers
+  constexpr float kLift = paged::kLift<kF16 && !kE4M3>, kGap = paged::kRescaleGap + kLift;
   constexpr int R = S::kRows, kSub = R / 16, kHeadsOf = 8 * kTiles;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* const ring = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -227,6 +228,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
   uint32_t qf[kTiles][D / 16][2];
   float o[kTiles][D / 16][4];
   float zs[kTiles][2], m_used[kTiles][2], l_run[kTiles][2];
+  // e4m3: the output is of weights times value scales, times 2^k of their own per head: w_up = 2^k, set so that w_max, the largest of
+  // them so far when it was set, came to 2^7
+  float w_max[kTiles][2], w_up[kTiles][2];
+  auto up_of = [](float w) { return __uint_as_float(static_cast<uint32_t>(min(261 - static_cast<int>(__float_as_uint(w) >> 23), 253)) << 23); };
   auto begin = [&]() {
     const int head0 = ((cur.block << heads_shift) + head_l) * group;
     const T* q = static_cast<const T*>(p.q) + cur.b * p.ld_q + static_cast<int64_t>(head0) * D;
@@ -274,6 +279,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
       for (int c = 0; c < 2; ++c) {
         m_used[n][c] = -INFINITY;
         l_run[n][c] = 0.f;
+        w_max[n][c] = 0.f;
+        w_up[n][c] = up_of(0.f);
       }
 #pragma unroll
       for (int i = 0; i < D / 16; ++i) o[n][i][0] = o[n][i][1] = o[n][i][2] = o[n][i][3] = 0.f;
@@ -321,7 +328,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             uint32_t w[4];
             ldmatrix_x4(w, (kb + k_off[j] + (k >> 2) * block_stride) ^ ((k & 3) * 32));
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) mma<kQkF16>(s[j][n], w, qf[n][k][0], qf[n][k][1]);
+            for (int n = 0; n < kTiles; ++n) mma<k16>(s[j][n], w, qf[n][k][0], qf[n][k][1]);
           }
         } else {
           uint32_t c[4];   // four codes of a key: dims 16 k + 4 t .. + 3 of keys 8 i + lane / 4
@@ -331,7 +338,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const uint32_t w[4] = {e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j])), e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j + 1])),
                                    e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j] >> 16)), e4m3x2_to_f16x2(static_cast<uint16_t>(c[2 * j + 1] >> 16))};
 #pragma unroll
-            for (int n = 0; n < kTiles; ++n) mma<kQkF16>(s[j][n], w, qf[n][k][0], qf[n][k][1]);
+            for (int n = 0; n < kTiles; ++n) mma<k16>(s[j][n], w, qf[n][k][0], qf[n][k][1]);
           }
         }
       }
@@ -375,7 +382,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         mx[n][c] = x * zs[n][c];
         need = need || mx[n][c] > m_used[n][c] + kGap;
       }
-    if (__any_sync(0xffffffffu, need)) {
+    const bool moved = __any_sync(0xffffffffu, need);
+    if (moved) {
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -384,8 +392,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
           if (x > m_used[n][c] + kGap) {
-            const float to = x - paged::kLift<kPvF16>, al = exp2_fast(m_used[n][c] - to);   // (the first time: 0)
+            const float to = x - kLift, al = exp2_fast(m_used[n][c] - to);   // (the first time: 0)
             m_used[n][c] = to;
+            if constexpr (kE4M3) w_max[n][c] *= al;
             l_run[n][c] *= al;
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
@@ -424,6 +433,44 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             e[j][n][2 * r + 1] *= x;
           }
         }
+      float top[kTiles][2];
+      bool grown = moved;
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          top[n][c] = fmaxf(fabsf(e[0][n][c]), fabsf(e[0][n][2 + c]));
+#pragma unroll
+          for (int j = 1; j < kSub; ++j) top[n][c] = fmaxf(top[n][c], fmaxf(fabsf(e[j][n][c]), fabsf(e[j][n][2 + c])));
+          grown = grown || top[n][c] * w_up[n][c] > 32768.f;
+        }
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            float x = top[n][c];
+#pragma unroll
+            for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+            w_max[n][c] = fmaxf(w_max[n][c], x);
+            const float up = up_of(w_max[n][c]);
+            // up / w_up, both powers of two (where that is out of range the output is 0 beside what comes)
+            const int k = 127 + static_cast<int>(__float_as_uint(up) >> 23) - static_cast<int>(__float_as_uint(w_up[n][c]) >> 23);
+            const float by = __uint_as_float(static_cast<uint32_t>(min(max(k, 0), 254)) << 23);
+            w_up[n][c] = up;
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) {
+              o[n][i][c] *= by;
+              o[n][i][2 + c] *= by;
+            }
+          }
+      }
+#pragma unroll
+      for (int j = 0; j < kSub; ++j)
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) e[j][n][x] *= w_up[n][x & 1];
     }
     uint32_t wt[kSub][kTiles][2];   // weights in 16 bits; their sum is that of the unrounded ones
 #pragma unroll
@@ -432,7 +479,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-          wt[j][n][r] = transposed(kPvF16 ? pack_f16(e[j][n][2 * r], e[j][n][2 * r + 1]) : pack_bf16(e[j][n][2 * r], e[j][n][2 * r + 1]));
+          wt[j][n][r] = transposed(k16 ? pack_f16(e[j][n][2 * r], e[j][n][2 * r + 1]) : pack_bf16(e[j][n][2 * r], e[j][n][2 * r + 1]));
     if (partial) {   // rows that nobody sees may hold anything, and 0 x NaN is NaN
       constexpr int kUnits = S::kRowBytes / 16, kUnitsOf = S::kBlockBytes / 16;
       for (int i = lane; i < R * kUnits; i += 32) {
@@ -451,7 +498,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
           uint32_t w[4];
           ldmatrix_x4_trans(w, (vb + v_off[j] + (i >> 2) * block_stride) ^ ((i & 3) * 32));
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, wt[j][n][0], wt[j][n][1]);
+          for (int n = 0; n < kTiles; ++n) mma<k16>(o[n][i], w, wt[j][n][0], wt[j][n][1]);
         }
       } else {
         // a word: dims 2 g4, 2 g4 + 1 of keys 2 t and 2 t + 1; the even dims are the tile's rows 0-7, the odd ones rows 8-15
@@ -459,12 +506,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         ldmatrix_x4_trans(c, (vb + v_off[0]) ^ (i * 16));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const uint32_t w[4] = {e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j], 0, 0x4420))),
-                                 e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j], 0, 0x4431))),
-                                 e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4420))),
-                                 e4m3x2_to_bf16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4431)))};
+          const uint32_t w[4] = {e4m3x2_to_f16x2(static_cast<uint16_t>(__byte_perm(c[2 * j], 0, 0x4420))),
+                                 e4m3x2_to_f16x2(static_cast<uint16_t>(__byte_perm(c[2 * j], 0, 0x4431))),
+                                 e4m3x2_to_f16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4420))),
+                                 e4m3x2_to_f16x2(static_cast<uint16_t>(__byte_perm(c[2 * j + 1], 0, 0x4431)))};
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) mma<kPvF16>(o[n][i], w, wt[j][n][0], wt[j][n][1]);
+          for (int n = 0; n < kTiles; ++n) mma<k16>(o[n][i], w, wt[j][n][0], wt[j][n][1]);
         }
       }
     }
@@ -485,11 +532,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
         if (g4 == 0) ml[warp * kHeadsOf + 8 * n + 2 * t4 + c] = make_float2(m_used[n][c], l_run[n][c]);
       }
     workers_sync();
-    float f[kTiles][2];
+    float f[kTiles][2], down[kTiles][2];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n)
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
+        down[n][c] = kE4M3 ? __uint_as_float((254u << 23) - __float_as_uint(w_up[n][c])) : 1.f;   // 1 / w_up
         const int row = 8 * n + 2 * t4 + c;
         // (each of the eight lanes of a head looks at one strip)
         const float2 mine = g4 < n_strips ? ml[((head_l << strip_shift) + g4) * kHeadsOf + row] : make_float2(-INFINITY, 0.f);
@@ -528,7 +576,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const int dim = kE4M3 ? 16 * i + 2 * g4 + (x >> 1) : 16 * i + g4 + 8 * (x >> 1);
-            mine[(8 * n + 2 * t4 + (x & 1)) * S::kMergePitch + dim] = o[n][S::kMergeDims / 16 * chunk + i][x] * f[n][x & 1];
+            mine[(8 * n + 2 * t4 + (x & 1)) * S::kMergePitch + dim] = o[n][S::kMergeDims / 16 * chunk + i][x] * f[n][x & 1] * down[n][x & 1];
           }
       meet();
       constexpr int kPairs = S::kMergeDims / 2;

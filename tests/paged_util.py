@@ -127,6 +127,8 @@ def check_attend(cache, out, lse, sink=0, window=0, sequences=None):
     With u_p the rounding of a weight to 16 bits (bf16 where the cache is e4m3), u_o that of the result, and weights p, values v:
       |out - ref| <= (u_p + 2 e) sum_s p_s |v_s| + u_o |ref|   (+ 2^-32 sum_s |v_s| where weights are fp16: a weight below 2^-14
     is rounded to a multiple of 2^-24; the largest weight of a part is at least 2^7 before the division)
+    e4m3 caches: weights times value scales are rounded to fp16, the largest of a part at least 2^7 when the others are: u_p is fp16's, and
+    2^-32 max_s (p_s scale_s) sum_s |code_s| is added for those that become subnormal.
     where e is the relative error of a weight before that rounding: that of its score, (d + 8) roundings of fp32 of products whose
     absolute sum is at most sum_i |q_i k_i| (a tree or a chain of fp32 additions, in log2 units, times ln 2), 2^-21 for exp2 and
     (n / 8 + 512) roundings for the chains of sums.  The log-sum-exp carries the score's error and the sum's.
@@ -136,7 +138,7 @@ def check_attend(cache, out, lse, sink=0, window=0, sequences=None):
     got, got_lse = to_np(out), to_np(lse)
     scale = cache.d ** -0.5
     u_o = UNIT[cache.dtype]
-    u_p = UNIT["bf16" if cache.e4m3 else cache.dtype]
+    u_p = UNIT["fp16" if cache.e4m3 else cache.dtype]
     group = cache.H // cache.G
     worst = 0.0
     for b in range(len(cache.lengths)) if sequences is None else sequences:
@@ -157,6 +159,9 @@ def check_attend(cache, out, lse, sink=0, window=0, sequences=None):
             tol = (u_p + 2 * e) * mass + u_o * np.abs(ref[h]) * (1 + u_p)
             if cache.dtype == "fp16" and not cache.e4m3:
                 tol = tol + 2.0 ** -32 * np.abs(v[rows, g]).sum(0)
+            if cache.e4m3:
+                vs = to_np(cache.v_scale)[rows, g]
+                tol = tol + 2.0 ** -32 * (p * vs).max() * np.abs(v[rows, g] / vs[:, None]).sum(0)
             if cache.dtype == "fp16":
                 tol = tol + 2.0 ** -25   # a result below 2^-14 is rounded to a multiple of 2^-24
             err = np.abs(got[b, h] - ref[h])

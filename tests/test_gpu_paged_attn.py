@@ -316,3 +316,22 @@ def test_two_contexts_on_two_streams(cuda_device):
     for c, (ctx, out, lse), (out1, lse1) in zip(cs, calls, first):
         assert ctx.status() == 0 and torch.equal(out, out1) and torch.equal(lse, lse1)
         pu.check_attend(c, out, lse)
+
+
+@pytest.mark.parametrize("shape", [(8, 1, 128, 128), (16, 1, 64, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_products_of_weights_and_scales_that_rise_and_fall(cuda_device, shape, dtype):
+    """e4m3: value scales that grow and shrink by more than fp16's range along a sequence, with scores that grow against them: what comes
+    to matter late must not be rounded by what mattered before."""
+    c = pu.Cache([1500, 1500], shape, 64, dtype, True, cuda_device, seed=27)
+    c.q[:] = 0
+    c.q[..., 0] = 1
+    c.k[:, 1:] = 0
+    c.k[:, 0] = torch.tensor([1.0], device=cuda_device).to(torch.float8_e4m3fn).view(torch.uint8)
+    for b, (score, scale) in enumerate([((0, 240), (60, -60)), ((0, 0), (-60, 14))]):   # in powers of two, first to last token
+        rows = torch.from_numpy(pu.orc.paged_rows(np.arange(1500), c.table[b], 64)).to(cuda_device)
+        c.k_scale[rows, 0] = torch.linspace(score[0], score[1], 1500, device=cuda_device) * (c.d ** 0.5 * 0.6931472)
+        c.v_scale[rows, 0] = torch.exp2(torch.linspace(scale[0], scale[1], 1500, device=cuda_device))
+    ctx, out, lse = pu.attend(c)
+    assert ctx.status() == 0
+    pu.check_attend(c, out, lse)
