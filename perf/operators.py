@@ -200,27 +200,31 @@ _contexts: dict = {}
 
 
 def _context(s):
-    """The library's handle, which a program keeps for the shapes that it serves."""
+    """The library's handle, which a program keeps per stream for the shapes that it serves (its calls go to the stream it was made for)."""
     from paper_2608_01662_b200 import binding
 
-    c = s["case"]
-    kv = binding.make_kv_params(n_heads=c["heads"], n_kv_heads=c["kv_heads"], d_qk=c["d_qk"], d_v=_d_v(c), latent=c["latent"], dtype=c["dtype"],
-                                e4m3=c["e4m3"], kv_page=c["page"], d_rope=c.get("d_rope", 0),
-                                rope_at=c["d_qk"] - 64 if c["latent"] and c["op"] == "append" else 0,
-                                rope_interleaved=c.get("interleaved", False), sink=c.get("sink", 0), window=c.get("window", 0),
-                                sm_scale=c["d_qk"] ** -0.5)
-    key = (bytes(kv), c["batch"])
-    if key not in _contexts:
-        _contexts[key] = binding.Context(None, 0, 0, c["batch"], device=s["q"].device, kv=kv)
-    return _contexts[key]
+    kv = s.get("kv")
+    if kv is None:
+        c = s["case"]
+        kv = s["kv"] = binding.make_kv_params(n_heads=c["heads"], n_kv_heads=c["kv_heads"], d_qk=c["d_qk"], d_v=_d_v(c), latent=c["latent"],
+                                              dtype=c["dtype"], e4m3=c["e4m3"], kv_page=c["page"], d_rope=c.get("d_rope", 0),
+                                              rope_at=c["d_qk"] - 64 if c["latent"] and c["op"] == "append" else 0,
+                                              rope_interleaved=c.get("interleaved", False), sink=c.get("sink", 0), window=c.get("window", 0),
+                                              sm_scale=c["d_qk"] ** -0.5)
+        s["kv_bytes"] = bytes(kv)
+    device = s["q"].device
+    stream = torch.cuda.current_stream(device)
+    key = (s["kv_bytes"], device, stream.cuda_stream)
+    ctx = _contexts.get(key)
+    if ctx is None:
+        ctx = _contexts[key] = binding.Context(None, 0, 0, device=device, stream=stream, kv=kv)
+    return ctx
 
 
 def run(state):
     s = state
     if own:
-        ctx = s.get("ctx")
-        if ctx is None:
-            ctx = s["ctx"] = _context(s)
+        ctx = _context(s)
         if s["case"]["op"] == "append":
             ctx.kv_append(s["k_new"], s["v_new"], s["k_pool"], s["v_pool"], s["page_table"], s["ctx_len"], s["ctx_len_out"],
                           tok_start=s["tok_start"], q=s["q"], q_out=s["q_out"], cos_sin=s["cos_sin"], k_scale=s["k_scale"], v_scale=s["v_scale"])
