@@ -48,7 +48,8 @@ __device__ __forceinline__ uint4 pack8(const float* x) {
 }
 // Eight codes of value / scale: round to nearest even, saturating.  inv is 1 / scale, correctly rounded; q = x inv, then q + (x - q scale) inv
 // with the remainder in one fma is then the correctly rounded quotient (Markstein 1990), a third of the instructions of a division
-// each.  (A quotient too small for that to hold is far below the smallest code.)
+// each.  The remainder is a multiple of the last places of q and scale and has to be a number of fp32, whose smallest is 2^-149: for the
+// quotients that codes are told apart by, from 2^-11 on, 2^-34 times a scale's 2^-113 still is.  For scales below 2^-90 it is divided.
 __device__ __forceinline__ uint2 codes8(const float* x, float scale, float inv) {
   uint32_t w[2];
 #pragma unroll
@@ -57,10 +58,10 @@ __device__ __forceinline__ uint2 codes8(const float* x, float scale, float inv) 
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       float2 v = make_float2(x[4 * h + 2 * j], x[4 * h + 2 * j + 1]);
-      if (inv >= 1.17549435e-38f && inv < INFINITY) {
+      if (inv >= 1.17549435e-38f && inv <= 0x1p90f) {
         const float p = v.x * inv, q = v.y * inv;
         v = make_float2(fmaf(fmaf(-p, scale, v.x), inv, p), fmaf(fmaf(-q, scale, v.y), inv, q));
-      } else {   // the reciprocal is not a normal number: a scale near either end of fp32, infinite or NaN
+      } else {   // a scale near either end of fp32 (its reciprocal is not a normal number, or the remainder none), infinite or NaN
         v = make_float2(__fdiv_rn(v.x, scale), __fdiv_rn(v.y, scale));
       }
       r |= static_cast<uint32_t>(__nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3)) << (16 * j);

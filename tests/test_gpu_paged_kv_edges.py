@@ -1,0 +1,42 @@
+"""lsa_kv_append and lsa_paged_attn at the ends of their ranges (needs a B200)."""
+import numpy as np
+import pytest
+import torch
+
+import paged_util as pu
+from oracle import lsa_oracle as orc
+from test_gpu_kv_append import make
+
+pytestmark = pytest.mark.gpu
+
+
+def test_codes_beside_midpoints_for_scales_of_every_size(cuda_device):
+    """e4m3 keys whose quotients by the scale lie at midpoints between codes, as near as fp32 values come to them, for scales from the
+    subnormal numbers up: the code is that of the fp32 quotient, as IEEE division rounds it.  No value here is rounded before: a key is a
+    power of two times an angle's cosine or sine."""
+    rng = np.random.default_rng(31)
+    exps = list(range(-128, -84)) + list(range(-80, 77, 12))
+    n, half = len(exps), 32
+    c, t, old = make((8, 2, 64, 64), [b + 1 for b in range(n)], [1] * n, 16, "bf16", True, cuda_device, True, 64, 0, False, seed=31)
+    want = np.zeros((n, 64), np.float32)
+    mids = np.array([(m + 0.5) / 8 * 2.0 ** e for m in range(8, 16) for e in range(-6, 8)] + [(m + 0.5) * 2.0 ** -9 for m in range(8)])
+    for b, e in enumerate(exps):
+        top = np.float32(448 * 2.0 ** (e + rng.random()))
+        scale = np.float32(top / np.float32(448))
+        near = (rng.choice(mids[mids < 440], 63) * np.float64(scale)).astype(np.float32)
+        want[b] = np.concatenate([[top], near * rng.choice([-1.0, 1.0], 63).astype(np.float32)])
+    up = 2.0 ** 40
+    t.k[:, :, :half] = 2.0 ** -40
+    t.k[:, :, half:] = 0
+    # (halves: dim j becomes x cos_j, dim j + 32 becomes x sin_j)
+    t.cos_sin = torch.from_numpy((want.astype(np.float64) * up).astype(np.float32)).to(cuda_device).contiguous()
+    ctx = t.append()
+    assert ctx.status() == 0
+    x = torch.from_numpy(want)
+    scale = x.abs().amax(-1) / 448
+    codes = (x / scale[:, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+    rows = [int(orc.paged_rows([b], c.table[b], 16)[0]) for b in range(n)]
+    for g in range(2):
+        assert torch.equal(c.k_scale[rows].cpu()[:, g], scale)
+        wrong = (c.k[rows].cpu()[:, 64 * g:64 * g + 64] != codes).any(1)
+        assert not bool(wrong.any()), [exps[b] for b in range(n) if wrong[b]]
