@@ -272,8 +272,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_consta
             const float2 f = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&qf[n][k][h]));
             qf[n][k][h] = pack_f16(f.x * up, f.y * up);
           }
-        zs[n][0] *= __shfl_sync(0xffffffffu, down, 8 * t4);
-        zs[n][1] *= __shfl_sync(0xffffffffu, down, 8 * t4 + 4);
+        // (not 0, however small: a hidden key's -inf times that is not -inf)
+        zs[n][0] = fmaxf(zs[n][0] * __shfl_sync(0xffffffffu, down, 8 * t4), 0x1p-149f);
+        zs[n][1] = fmaxf(zs[n][1] * __shfl_sync(0xffffffffu, down, 8 * t4 + 4), 0x1p-149f);
       }
 #pragma unroll
       for (int c = 0; c < 2; ++c) {

@@ -40,3 +40,15 @@ def test_codes_beside_midpoints_for_scales_of_every_size(cuda_device):
         assert torch.equal(c.k_scale[rows].cpu()[:, g], scale)
         wrong = (c.k[rows].cpu()[:, 64 * g:64 * g + 64] != codes).any(1)
         assert not bool(wrong.any()), [exps[b] for b in range(n) if wrong[b]]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_scales_of_scores_that_underflow(cuda_device, dtype):
+    """e4m3: sm_scale times a query's size is far below the smallest fp32 number, so every seen token weighs the same; the hidden ones at
+    the end of a strip nothing."""
+    c = pu.Cache([1, 50, 77, 300, 2000], (8, 2, 64, 64), 16, dtype, True, cuda_device, seed=32, poison=True)
+    c.q *= 2.0 ** (-90 if dtype == "bf16" else -10)
+    ctx, out, lse = pu.attend(c, sm_scale=2.0 ** -90)
+    assert ctx.status() == 0
+    c.q.zero_()      # the same weights: scores of 0
+    pu.check_attend(c, out, lse)
