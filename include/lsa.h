@@ -395,8 +395,9 @@ typedef struct {
 
 enum { LSA_DTYPE_BF16 = 0, LSA_DTYPE_FP16 = 1 };
 
-/* Scratch of lsa_paged_attn with these parameters (lsa_kv_append needs the 256 bytes of the status words only): partial
- * results of the parts that a cache's length is split into.  It does not grow with the batch.  Writes *bytes (host). */
+/* Scratch of lsa_paged_attn with these parameters (lsa_kv_append needs the 256 bytes of the status words only, a context without any
+ * workspace is refused with LSA_ERR_WORKSPACE): partial results of the parts that a cache's length is split into.  It does not grow with
+ * the batch.  Writes *bytes (host). */
 LSA_API int lsa_kv_workspace_bytes(const lsa_kv_params* p, size_t* bytes);
 
 /* New tokens into the cache.  Token i of sequence b goes to position pos = ctx_len[b] + i - its sequence's first token; its key

@@ -932,6 +932,7 @@ int lsa_kv_append(lsa_ctx* c, const lsa_kv_params* p, const void* k_new, int64_t
   if (c == nullptr) return LSA_ERR_ARG;   // (last: the arguments are judged without a device)
   if (batch == 0) return LSA_OK;
   if (n_tok == 0 && ctx_len_out == nullptr) return LSA_OK;
+  if (c->ws == nullptr) return LSA_ERR_WORKSPACE;   // (tokens that find no place would be lost without a word)
   const OnDevice device(c->device);
   if (device.error() != cudaSuccess) return cuda_fail(c, device.error());
   lsa::KvAppendArgs a{};

@@ -5,6 +5,7 @@ import torch
 
 import paged_util as pu
 from oracle import lsa_oracle as orc
+from paper_2608_01662_b200 import binding
 from test_gpu_kv_append import make
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +53,21 @@ def test_scales_of_scores_that_underflow(cuda_device, dtype):
     assert ctx.status() == 0
     c.q.zero_()      # the same weights: scores of 0
     pu.check_attend(c, out, lse)
+
+
+def test_append_without_a_workspace_is_refused(cuda_device):
+    """Tokens that find no place are reported through words in the workspace: without one nobody would learn of them."""
+    import ctypes
+
+    c, t, old = make((8, 2, 64, 64), [9, 20], [1, 1], 16, "bf16", False, cuda_device, True, 32, 0, False, seed=33)
+    ctx = t.append()
+    bare = ctypes.c_void_p()
+    assert binding.lib().lsa_create(ctypes.byref(bare), cuda_device.index or 0, ctypes.c_void_p(ctx.stream.cuda_stream), None, 0) == 0
+    with_workspace, ctx.h = ctx.h, bare
+    try:
+        with pytest.raises(binding.LsaError) as e:
+            t.append(ctx)
+        assert e.value.code == -3
+    finally:
+        ctx.h = with_workspace
+        binding.lib().lsa_destroy(bare)
