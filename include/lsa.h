@@ -437,6 +437,9 @@ LSA_API int lsa_kv_append(lsa_ctx* ctx, const lsa_kv_params* p, const void* k_ne
  * The cached tokens of all sequences are dealt evenly to the SMs, and parts of a sequence are joined by their log-sum-exps (in
  * a fixed order: the same call gives the same bits).  A sequence's rounding depends on the batch that it is dealt with.  The parts
  * lie in the context's workspace: calls of one context, and graphs captured from them, must not run at the same time.
+ * Tiles are numbered in 32 bits, counted as if every sequence filled its row of the table: where batch * (page_table_stride * kv_page / t + 2)
+ * * (n_kv_heads / u) is above 2^31 - 161 the call is refused with LSA_ERR_SHAPE; u is the largest of 8, 4, 2 and 1 that divides n_kv_heads,
+ * t = 128 / u (latent rows: 64).  For 8 KV heads that is a table for 2^35 tokens in all.
  * A length outside [0, page_table_stride * kv_page] (it is clamped to that range) or a page number outside [0, n_pages) (its tokens count
  * as zero rows) is reported as LSA_ERR_INDEX by lsa_status; other sequences are not affected. */
 LSA_API int lsa_paged_attn(lsa_ctx* ctx, const lsa_kv_params* p, const void* q, int64_t ld_q, const void* k_pool, int64_t ld_k,

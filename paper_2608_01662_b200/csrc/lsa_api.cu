@@ -961,6 +961,8 @@ int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld
   if (batch > 0 && (q == nullptr || out == nullptr)) return LSA_ERR_ARG;
   if (!aligned16(q) || !aligned16(out) || ld_q % 8 != 0 || ld_out % 8 != 0) return LSA_ERR_SHAPE;
   if (ld_q < static_cast<int64_t>(p->n_heads) * p->d_qk || ld_out < static_cast<int64_t>(p->n_heads) * p->d_v) return LSA_ERR_SHAPE;
+  // (the kernels number the tiles of all sequences, as long as their tables' rows, in 32 bits)
+  if (batch > ((1ll << 31) - lsa::kMaxPagedUnits - 1) / lsa::paged_entries(p->latent, p->n_kv_heads, page_table_stride * p->kv_page)) return LSA_ERR_SHAPE;
   if (c == nullptr) return LSA_ERR_ARG;
   if (batch == 0) return LSA_OK;
   const KvScratch s = kv_scratch(p);
@@ -981,7 +983,6 @@ int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld
   a.scale2 = p->sm_scale * 1.4426950408889634f;
   a.q = q; a.k_pool = k_pool; a.v_pool = v_pool; a.k_scale = k_scale; a.v_scale = v_scale;
   a.page_table = page_table; a.ctx_len = ctx_len; a.out = out; a.lse = lse;
-  if (lsa::paged_entries(a) >= (1ll << 31) - a.units) return LSA_ERR_SHAPE;   // (2^35 tokens and more)
   a.part_out = reinterpret_cast<float*>(c->ws + s.part_out);
   a.part_lse = reinterpret_cast<float*>(c->ws + s.part_lse);
   a.parts = reinterpret_cast<int4*>(c->ws + s.parts);

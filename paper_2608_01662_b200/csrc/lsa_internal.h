@@ -266,8 +266,8 @@ struct PagedAttnArgs {
 constexpr int kMaxPagedUnits = 160;     // one block per SM: the scratch is sized for that many
 // query heads that a unit works on at a time (rows of its partial results)
 int paged_rows(int latent, int H, int G);
-// entries of the list at most: tiles of `batch` sequences of max_len tokens, times the blocks of KV heads
-int64_t paged_entries(const PagedAttnArgs& a);
+// entries of the list that a sequence of max_len tokens may have: its tiles, times the blocks of KV heads
+int64_t paged_entries(int latent, int G, int64_t max_len);
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch);      // separate keys and values
 cudaError_t launch_paged_attn_tc(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch);   // latent rows
 

@@ -818,9 +818,9 @@ cudaError_t launch_d(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch)
 }  // namespace
 
 int paged_rows(int latent, int H, int G) { return latent ? 64 : (H / G) << heads_shift_of(G); }
-int64_t paged_entries(const PagedAttnArgs& a) {
-  const int hs = heads_shift_of(a.G), keys = a.latent ? 64 : 16 << (3 - hs);   // (at least so many keys a tile)
-  return static_cast<int64_t>(a.batch) * (a.max_len / keys + 2) * (a.G >> hs);
+int64_t paged_entries(int latent, int G, int64_t max_len) {
+  const int hs = heads_shift_of(G), keys = latent ? 64 : 16 << (3 - hs);   // (at least so many keys a tile)
+  return (max_len / keys + 2) * (G >> hs);
 }
 
 cudaError_t launch_paged_attn(const PagedAttnArgs& a, cudaStream_t st, int64_t* n_launch) {

@@ -188,3 +188,16 @@ def test_binding_looks_at_page_tables():
         with pytest.raises(binding.LsaError) as e:
             binding._kv_table(bad, "t")
         assert e.value.code == -1
+
+
+@pytest.mark.parametrize("which,u,t", [(MLA, 1, 64), (GQA, 8, 16), (dict(GQA, n_heads=128, n_kv_heads=128), 8, 16), (dict(GQA, n_heads=4096, n_kv_heads=4096), 8, 16),
+                                       (dict(GQA, n_heads=6, n_kv_heads=6), 2, 64), (dict(GQA, n_heads=3, n_kv_heads=3), 1, 128)])
+@pytest.mark.parametrize("pages", [1, 100, 65536, (1 << 31) // 256 - 8])
+def test_tiles_are_numbered_in_32_bits(which, u, t, pages):
+    """Both sides of the most sequences that a call takes, by the widths of their tables (no context: what is accepted ends with -1)."""
+    kv = binding.make_kv_params(**which)
+    kv.kv_page = 256
+    most = (2 ** 31 - 161) // ((pages * 256 // t + 2) * (kv.n_kv_heads // u))
+    assert _attn(kv, stride=pages, batch=min(most, 2 ** 31 - 1)) == -1
+    if most < 2 ** 31 - 1:
+        assert _attn(kv, stride=pages, batch=most + 1) == -2 and _attn(kv, stride=pages, batch=2 ** 31 - 1) == -2
