@@ -236,9 +236,11 @@ class Context:
     def __init__(self, params: LsaParams | None, n_query: int, n_key_max: int, batch: int = 1, device=None, stream=None,
                  kv: LsaKvParams | None = None):
         """params: the sparse path's (None: the context serves kv_append and paged_attn only); kv: those calls' parameters."""
+        if params is None and kv is None:
+            raise LsaError(-1, "Context", "neither the sparse path's parameters nor those of a key-value cache")
         self.params, self.kv = params, kv
         self.device = torch.device(device if device is not None else "cuda:0")
-        nbytes = workspace_bytes(params, n_query, n_key_max, batch) if params is not None or kv is None else 0
+        nbytes = workspace_bytes(params, n_query, n_key_max, batch) if params is not None else 0
         if kv is not None:
             nbytes = max(nbytes, kv_workspace_bytes(kv))
             # what every call needs of them (an attribute of a ctypes structure costs more than one of an object)
@@ -266,6 +268,13 @@ class Context:
     def _chk(self, r, where):
         if r != 0:
             raise LsaError(r, where, lib().lsa_last_cuda_error(self.h).decode())
+
+    def _sparse(self, where, params=None):
+        """A sparse call's parameters: its own, or the context's."""
+        params = params if params is not None else self.params
+        if params is None:
+            raise LsaError(-1, where, "the context was made without the sparse path's parameters")
+        return ctypes.byref(params)
 
     def status(self) -> int:
         out = c_int(0)
@@ -295,20 +304,20 @@ class Context:
     def block_means(self, k_idx, k_scale, n_key, kmean, page_table=None, ctx_len=None):
         pt_stride = page_table.shape[1] if page_table is not None else 0
         batch = page_table.shape[0] if page_table is not None else 1
-        self._chk(lib().lsa_block_means(self.h, ctypes.byref(self.params), _p(k_idx), _p(k_scale), n_key,
+        self._chk(lib().lsa_block_means(self.h, self._sparse("lsa_block_means"), _p(k_idx), _p(k_scale), n_key,
                                         _p(page_table), pt_stride, _p(ctx_len), batch, _p(kmean)), "lsa_block_means")
 
     def index(self, q_idx, w, k_idx, k_scale, kmean, q_pos0, n_query, n_key, sparse_idx, n_sparse, pages_out=None,
               page_table=None, ctx_len=None):
         pt_stride = page_table.shape[1] if page_table is not None else 0
         batch = page_table.shape[0] if page_table is not None else 1
-        self._chk(lib().lsa_index(self.h, ctypes.byref(self.params), _p(q_idx), _p(w), _p(k_idx), _p(k_scale),
+        self._chk(lib().lsa_index(self.h, self._sparse("lsa_index"), _p(q_idx), _p(w), _p(k_idx), _p(k_scale),
                                   _p(kmean), q_pos0, n_query, n_key, _p(page_table), pt_stride, _p(ctx_len), batch,
                                   _p(sparse_idx), _p(n_sparse), _p(pages_out)), "lsa_index")
 
     def select(self, scores, cand_pos, q_pos0, k, apply_range, idx_out, n_out):
         n_query, n_cand = scores.shape
-        self._chk(lib().lsa_select(self.h, ctypes.byref(self.params), _p(scores), scores.stride(0), _p(cand_pos),
+        self._chk(lib().lsa_select(self.h, self._sparse("lsa_select"), _p(scores), scores.stride(0), _p(cand_pos),
                                    q_pos0, n_query, n_cand, k, 1 if apply_range else 0, _p(idx_out), _p(n_out)),
                   "lsa_select")
 
@@ -316,42 +325,40 @@ class Context:
                 ctx_len=None):
         pt_stride = page_table.shape[1] if page_table is not None else 0
         batch = page_table.shape[0] if page_table is not None else 1
-        self._chk(lib().lsa_convert(self.h, ctypes.byref(self.params), _p(sparse_idx), _p(n_sparse), q_pos0, n_query,
+        self._chk(lib().lsa_convert(self.h, self._sparse("lsa_convert"), _p(sparse_idx), _p(n_sparse), q_pos0, n_query,
                                     _p(page_table), pt_stride, _p(ctx_len), batch, _p(rows_out), _p(n_rows_out),
                                     _p(runs_out)), "lsa_convert")
 
     def sparse_attn(self, q, k, v, sparse_idx, n_sparse, q_pos0, n_query, n_key, out, lse=None, rows=None,
                     n_rows=None, ctx_len=None, batch=1, params=None):
-        prm = params if params is not None else self.params
-        self._chk(lib().lsa_sparse_attn(self.h, ctypes.byref(prm), _p(q), _p(k), _p(v), k.stride(0),
+        self._chk(lib().lsa_sparse_attn(self.h, self._sparse("lsa_sparse_attn", params), _p(q), _p(k), _p(v), k.stride(0),
                                         v.stride(0), _p(sparse_idx), _p(n_sparse), _p(rows), _p(n_rows), q_pos0,
                                         n_query, n_key, _p(ctx_len), batch, _p(out), _p(lse)), "lsa_sparse_attn")
 
     def append(self, k_new, k_idx, k_scale, kmean, page_table, ctx_len, ctx_len_out=None, kv_new=(), kv_pool=()):
         batch = page_table.shape[0]
         row_bytes = kv_pool[0].stride(0) * kv_pool[0].element_size() if len(kv_pool) else 0
-        self._chk(lib().lsa_append(self.h, ctypes.byref(self.params), _p(k_new), _p(k_idx), _p(k_scale), _p(kmean),
+        self._chk(lib().lsa_append(self.h, self._sparse("lsa_append"), _p(k_new), _p(k_idx), _p(k_scale), _p(kmean),
                                    _p(page_table), page_table.shape[1], _p(ctx_len), batch, _p(ctx_len_out),
                                    len(kv_pool), _parr(list(kv_new)) if len(kv_pool) else None,
                                    _parr(list(kv_pool)) if len(kv_pool) else None, row_bytes), "lsa_append")
 
     def merge(self, outs, lses, n_query, out, lse=None, params=None):
-        prm = params if params is not None else self.params
-        self._chk(lib().lsa_merge(self.h, ctypes.byref(prm), len(outs), _parr(outs), _parr(lses), n_query, _p(out),
+        self._chk(lib().lsa_merge(self.h, self._sparse("lsa_merge", params), len(outs), _parr(outs), _parr(lses), n_query, _p(out),
                                   _p(lse)), "lsa_merge")
 
     def layer_group(self, q_idx, w, k_idx, k_scale, kmean, q_pos0, n_query, n_key, q, k, v, out, lse, sparse_idx,
                     n_sparse, page_table=None, ctx_len=None):
         pt_stride = page_table.shape[1] if page_table is not None else 0
         batch = page_table.shape[0] if page_table is not None else 1
-        self._chk(lib().lsa_layer_group(self.h, ctypes.byref(self.params), _p(q_idx), _p(w), _p(k_idx), _p(k_scale),
+        self._chk(lib().lsa_layer_group(self.h, self._sparse("lsa_layer_group"), _p(q_idx), _p(w), _p(k_idx), _p(k_scale),
                                         _p(kmean), q_pos0, n_query, n_key, _p(page_table), pt_stride, _p(ctx_len),
                                         batch, _parr(q), _parr(k), _parr(v), k[0].stride(0), v[0].stride(0),
                                         _parr(out), _parr(lse), _p(sparse_idx), _p(n_sparse)), "lsa_layer_group")
 
     def layer_group_host(self, q_idx_host, w_host, k_idx, k_scale, kmean, q_pos0, n_query, n_key, q_host, k, v, out_host,
                          stage_queries, stage):
-        self._chk(lib().lsa_layer_group_host(self.h, ctypes.byref(self.params), _p(q_idx_host), _p(w_host), _p(k_idx),
+        self._chk(lib().lsa_layer_group_host(self.h, self._sparse("lsa_layer_group_host"), _p(q_idx_host), _p(w_host), _p(k_idx),
                                              _p(k_scale), _p(kmean), q_pos0, n_query, n_key, _parr(q_host), _parr(k),
                                              _parr(v), k[0].stride(0), v[0].stride(0), _parr(out_host), stage_queries,
                                              _parr(stage), stage[0].numel()), "lsa_layer_group_host")

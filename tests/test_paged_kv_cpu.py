@@ -201,3 +201,20 @@ def test_tiles_are_numbered_in_32_bits(which, u, t, pages):
     assert _attn(kv, stride=pages, batch=min(most, 2 ** 31 - 1)) == -1
     if most < 2 ** 31 - 1:
         assert _attn(kv, stride=pages, batch=most + 1) == -2 and _attn(kv, stride=pages, batch=2 ** 31 - 1) == -2
+
+
+def test_sparse_calls_of_a_context_without_their_parameters_are_refused():
+    ctx = binding.Context.__new__(binding.Context)
+    ctx.h, ctx.params, ctx.kv = None, None, binding.make_kv_params(**MLA)
+    t = torch.zeros(4, 4)
+    calls = [lambda: ctx.block_means(t, t, 4, t), lambda: ctx.index(t, t, t, t, t, 0, 4, 4, t, t), lambda: ctx.select(t, t, 0, 4, True, t, t),
+             lambda: ctx.convert(t, t, 0, 4, t, t), lambda: ctx.sparse_attn(t, t, t, t, t, 0, 4, 4, t), lambda: ctx.append(t, t, t, t, t, t),
+             lambda: ctx.merge([t], [t], 4, t), lambda: ctx.layer_group(t, t, t, t, t, 0, 4, 4, [t], [t], [t], [t], [t], t, t),
+             lambda: ctx.layer_group_host(t, t, t, t, t, 0, 4, 4, [t], [t], [t], [t], 4, [t])]
+    for call in calls:
+        with pytest.raises(binding.LsaError) as e:
+            call()
+        assert e.value.code == -1
+    with pytest.raises(binding.LsaError) as e:
+        binding.Context(None, 0, 0)
+    assert e.value.code == -1
