@@ -221,13 +221,19 @@ def index_static(params: LsaParams, q_idx, w, k_idx, k_scale, kmean, q_pos0, n_q
 
 def index_static_status(device, stream=None) -> int:
     """lsa_index_static_status: waits for the stream, returns and clears the status word of lsa_index_static."""
-    dev = torch.device(device)
+    dev = _numbered(device)
     stream = stream if stream is not None else torch.cuda.current_stream(dev)
     st = c_int(0)
-    r = lib().lsa_index_static_status(dev.index or 0, c_void_p(stream.cuda_stream), ctypes.byref(st))
+    r = lib().lsa_index_static_status(dev.index, c_void_p(stream.cuda_stream), ctypes.byref(st))
     if r != 0:
         raise LsaError(r, "lsa_index_static_status")
     return st.value
+
+
+def _numbered(device) -> torch.device:
+    """A CUDA device with its number: one without ("cuda") is the current one, as it is where tensors are made."""
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
 
 
 class Context:
@@ -239,7 +245,7 @@ class Context:
         if params is None and kv is None:
             raise LsaError(-1, "Context", "neither the sparse path's parameters nor those of a key-value cache")
         self.params, self.kv = params, kv
-        self.device = torch.device(device if device is not None else "cuda:0")
+        self.device = _numbered(device if device is not None else "cuda:0")
         nbytes = workspace_bytes(params, n_query, n_key_max, batch) if params is not None else 0
         if kv is not None:
             nbytes = max(nbytes, kv_workspace_bytes(kv))
@@ -248,11 +254,11 @@ class Context:
             self._kv_dtype = tuple(_KV_DTYPES.values())[kv.dtype]
             self._kv_codes = {torch.float8_e4m3fn: torch.float8_e4m3fn} if kv.cache_e4m3 else None   # (else bytes)
             self._kv_k, self._kv_v, self._kv_q, self._kv_o = (kv.n_kv_heads, kv.d_qk), (kv.n_kv_heads, kv.d_v), (kv.n_heads, kv.d_qk), (kv.n_heads, kv.d_v)
-            self._kv_dev, self._kv_append, self._paged_attn = self.device.index or 0, lib().lsa_kv_append, lib().lsa_paged_attn
+            self._kv_dev, self._kv_append, self._paged_attn = self.device.index, lib().lsa_kv_append, lib().lsa_paged_attn
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
         h = c_void_p()
-        r = lib().lsa_create(ctypes.byref(h), self.device.index or 0, c_void_p(self.stream.cuda_stream),
+        r = lib().lsa_create(ctypes.byref(h), self.device.index, c_void_p(self.stream.cuda_stream),
                              c_void_p(self.workspace.data_ptr()), nbytes)
         if r != 0:
             raise LsaError(r, "lsa_create")

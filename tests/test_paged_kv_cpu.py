@@ -218,3 +218,21 @@ def test_sparse_calls_of_a_context_without_their_parameters_are_refused():
     with pytest.raises(binding.LsaError) as e:
         binding.Context(None, 0, 0)
     assert e.value.code == -1
+
+
+def test_a_device_without_a_number_is_the_current_one(monkeypatch):
+    """The context, its workspace and the tensors that its calls take are on one device, also where that is not the first."""
+    from types import SimpleNamespace
+
+    made, real = [], binding.lib()
+    empty = torch.empty
+    fake = SimpleNamespace(lsa_kv_workspace_bytes=real.lsa_kv_workspace_bytes, lsa_kv_append=None, lsa_paged_attn=None, lsa_destroy=lambda h: 0,
+                           lsa_create=lambda h, device, *rest: made.append(device) or 0)
+    monkeypatch.setattr(binding, "lib", lambda: fake)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: SimpleNamespace(cuda_stream=0))
+    monkeypatch.setattr(torch, "empty", lambda n, dtype, device: made.append(torch.device(device)) or empty(8, dtype=dtype))
+    for device, index in (("cuda", 3), (torch.device("cuda"), 3), ("cuda:1", 1), (None, 0)):
+        made.clear()
+        ctx = binding.Context(None, 0, 0, device=device, kv=binding.make_kv_params(**GQA))
+        assert made == [torch.device("cuda", index), index] and ctx._kv_dev == index
