@@ -298,7 +298,8 @@ cudaError_t launch_t(const KvAppendArgs& a, cudaStream_t st) {
   constexpr int kFew = kFewTokens<D>, kMany = kManyTokens<D>, kRows = kMany / (D / 16);   // rows of the smaller block at a time
   const int rows = std::max(a.q != nullptr ? a.H : 0, a.latent ? 1 : 2 * a.G);
   if (a.n_tok <= a.sm_count && rows > 4 * kRows) return launch_pdl(kv_append_kernel<T, D, kE4M3, kFew, 4>, grid, dim3(kFew), 0, st, a);
-  if (D == 576 && rows <= 2 * kRows) return launch_pdl(kv_append_kernel<T, D, kE4M3, kMany, 2>, grid, dim3(kMany), 0, st, a);
+  if constexpr (D == 576)
+    if (rows <= 2 * kRows) return launch_pdl(kv_append_kernel<T, D, kE4M3, kMany, 2>, grid, dim3(kMany), 0, st, a);
   return launch_pdl(kv_append_kernel<T, D, kE4M3, kMany, 4>, grid, dim3(kMany), 0, st, a);
 }
 template <typename T>
