@@ -26,10 +26,6 @@ struct lsa_ctx {
   int n_host_slots;
   // per-kernel timing (lsa_profile_*): event pairs recorded around the launches of each kernel class
   int tune[LSA_TUNE_COUNT];
-  // Row lists of the last kernel launched through this context, if that kernel was a paged attention launch: the next
-  // attention launch on the same lists may read them ahead of its programmatic dependency wait (the lists were
-  // complete before that last kernel started).  Any other launch through the context clears it.
-  const void* last_attn_rows;
   int prof_on;
   int prof_n;
   cudaEvent_t* prof_ev;   // 2 * kProfPairs events, created on first enable
@@ -50,7 +46,6 @@ constexpr int64_t kFlatFusedMaxKeys = 4096;   // caches up to this length: the f
 template <class F>
 cudaError_t timed(lsa_ctx* c, int cat, F launch) {
   const bool rec = c->prof_on && c->prof_ev != nullptr && c->prof_n < kProfPairs;
-  if (cat != LSA_K_ATTN) c->last_attn_rows = nullptr;
   if (rec) cudaEventRecord(c->prof_ev[2 * c->prof_n], c->stream);
   const cudaError_t e = launch();
   if (rec) {
@@ -377,10 +372,14 @@ int run_index(lsa_ctx* c, const lsa_params* p, const void* q_idx, const float* w
   return LSA_OK;
 }
 
+// follows_layer: the launch before this one on the stream was the attention of another layer of the same group, from the same library
+// call.  Only then are the row lists and the caches known to have been complete before that launch began, so that this one may
+// read them ahead of its programmatic dependency wait: whatever else the stream holds (an append through another context, a
+// copy of the caller's) may have been launched to write them, and may not have finished.
 int run_attn(lsa_ctx* c, const lsa_params* p, const void* q, const void* k, const void* v, int64_t ld_k,
              int64_t ld_v, const int32_t* sparse_idx, const int32_t* n_sparse, const int32_t* rows,
              const int32_t* n_rows, int64_t q_pos0, int64_t n_query, const int32_t* ctx_len, int batch,
-             void* out, float* lse, int64_t n_key = 0) {
+             void* out, float* lse, int64_t n_key, bool follows_layer) {
   const int64_t nq = p->paged ? batch : n_query;
   if (nq == 0) return LSA_OK;
   lsa::AttnArgs a{};
@@ -394,7 +393,7 @@ int run_attn(lsa_ctx* c, const lsa_params* p, const void* q, const void* k, cons
   a.n_split = 1; a.sm_count = c->sm_count; a.status = status_word(c);
   a.qk_waits_pv = c->tune[LSA_TUNE_ATTN_PV_WAIT];
   a.gather4 = c->tune[LSA_TUNE_ATTN_GATHER];
-  a.rows_stable = rows != nullptr && c->last_attn_rows == rows;
+  a.rows_stable = follows_layer && rows != nullptr;
   const bool use_tc = c->tune[LSA_TUNE_ATTN_TC] && lsa::attn_tc_supported(a);
   if (p->paged) {
     const WsLayout l = ws_layout(p, nq, 0, batch);
@@ -414,7 +413,6 @@ int run_attn(lsa_ctx* c, const lsa_params* p, const void* q, const void* k, cons
   cudaError_t e = timed(c, LSA_K_ATTN, [&] {
     return use_tc ? lsa::launch_attn_tc(a, c->stream, &c->launches) : lsa::launch_attn(a, c->stream, &c->launches);
   });
-  c->last_attn_rows = (e == cudaSuccess && use_tc && p->paged) ? rows : nullptr;
   if (e == cudaSuccess && a.n_split > 1 && !use_tc) e = timed(c, LSA_K_MERGE, [&] { return lsa::launch_merge(a, c->stream, &c->launches); });
   return e == cudaSuccess ? LSA_OK : cuda_fail(c, e);
 }
@@ -670,10 +668,10 @@ int lsa_convert(lsa_ctx* c, const lsa_params* p, const int32_t* sparse_idx, cons
   return e == cudaSuccess ? LSA_OK : cuda_fail(c, e);
 }
 
-int lsa_sparse_attn(lsa_ctx* c, const lsa_params* p, const void* q, const void* k, const void* v, int64_t ld_k,
-                    int64_t ld_v, const int32_t* sparse_idx, const int32_t* n_sparse, const int32_t* rows,
-                    const int32_t* n_rows, int64_t q_pos0, int64_t n_query, int64_t n_key, const int32_t* ctx_len,
-                    int batch, void* out, float* lse) {
+static int attn_checked(lsa_ctx* c, const lsa_params* p, const void* q, const void* k, const void* v, int64_t ld_k,
+                        int64_t ld_v, const int32_t* sparse_idx, const int32_t* n_sparse, const int32_t* rows,
+                        const int32_t* n_rows, int64_t q_pos0, int64_t n_query, int64_t n_key, const int32_t* ctx_len,
+                        int batch, void* out, float* lse, bool follows_layer) {
   if (c == nullptr) return LSA_ERR_ARG;
   int r = check_params(p, false, true);
   if (r != LSA_OK) return r;
@@ -684,7 +682,14 @@ int lsa_sparse_attn(lsa_ctx* c, const lsa_params* p, const void* q, const void* 
   if (n_query < 0 || q_pos0 < 0 || n_key < 0) return LSA_ERR_ARG;
   if (ld_k < p->d_qk || ld_v < p->d_v || (ld_k % 8) || (ld_v % 8)) return LSA_ERR_SHAPE;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return LSA_ERR_SHAPE;
-  return run_attn(c, p, q, k, v, ld_k, ld_v, sparse_idx, n_sparse, rows, n_rows, q_pos0, n_query, ctx_len, batch, out, lse, n_key);
+  return run_attn(c, p, q, k, v, ld_k, ld_v, sparse_idx, n_sparse, rows, n_rows, q_pos0, n_query, ctx_len, batch, out, lse, n_key, follows_layer);
+}
+
+int lsa_sparse_attn(lsa_ctx* c, const lsa_params* p, const void* q, const void* k, const void* v, int64_t ld_k,
+                    int64_t ld_v, const int32_t* sparse_idx, const int32_t* n_sparse, const int32_t* rows,
+                    const int32_t* n_rows, int64_t q_pos0, int64_t n_query, int64_t n_key, const int32_t* ctx_len,
+                    int batch, void* out, float* lse) {
+  return attn_checked(c, p, q, k, v, ld_k, ld_v, sparse_idx, n_sparse, rows, n_rows, q_pos0, n_query, n_key, ctx_len, batch, out, lse, false);
 }
 
 int lsa_merge(lsa_ctx* c, const lsa_params* p, int n_parts, const void* const* outs, const float* const* lses,
@@ -731,8 +736,8 @@ int lsa_layer_group(lsa_ctx* c, const lsa_params* p, const void* q_idx, const fl
   // The layers run one after another on the stream: in a model the query of layer r + 1 is computed from the output of
   // layer r, so they are never launched side by side.
   for (int i = 0; i < p->n_layers; ++i) {
-    r = lsa_sparse_attn(c, p, q[i], k[i], v[i], ld_k, ld_v, sparse_idx, n_sparse, rows, n_rows, q_pos0, n_query,
-                        n_key, ctx_len, batch, out[i], lse ? lse[i] : nullptr);
+    r = attn_checked(c, p, q[i], k[i], v[i], ld_k, ld_v, sparse_idx, n_sparse, rows, n_rows, q_pos0, n_query,
+                     n_key, ctx_len, batch, out[i], lse ? lse[i] : nullptr, i > 0);
     if (r != LSA_OK) return r;
   }
   return LSA_OK;
@@ -987,7 +992,6 @@ int lsa_paged_attn(lsa_ctx* c, const lsa_kv_params* p, const void* q, int64_t ld
   a.part_lse = reinterpret_cast<float*>(c->ws + s.part_lse);
   a.parts = reinterpret_cast<int4*>(c->ws + s.parts);
   a.status = status_word(c); a.notice = notice_word(c);
-  c->last_attn_rows = nullptr;   // (the launch before the next sparse one is no longer one on its row lists)
   const cudaError_t e = timed(c, LSA_K_ATTN, [&] {
     return p->latent ? lsa::launch_paged_attn_tc(a, c->stream, &c->launches) : lsa::launch_paged_attn(a, c->stream, &c->launches);
   });

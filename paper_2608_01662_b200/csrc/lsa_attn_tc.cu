@@ -279,9 +279,9 @@ __global__ void __launch_bounds__(Warps<kRows>::kThreads, 1) sparse_attn_tc_kern
   // Programmatic dependent launch: this block may have been placed while the previous kernel of the stream was still
   // draining; what that kernel wrote is read, and what it may still read is overwritten, only after
   // griddepcontrol.wait.  The next kernel's blocks may be placed from then on.
-  // rows_stable: the row lists (and the caches, as always) were complete before the previous kernel started, so the
-  // gather warps read them and put the first two key tiles in flight while that kernel drains, and wait only before
-  // they request Q; every other thread waits here.
+  // rows_stable (the layers of a group after its first): the row lists and the caches were complete before the previous kernel
+  // started, so the gather warps read them and put the first two key tiles in flight while that kernel drains, and wait only
+  // before they request Q; every other thread waits here.
   const bool early_rows = kRows && p.rows_stable != 0 && q_tma != 0;   // block-uniform
   auto dependency_wait = [&]() {
     asm volatile("griddepcontrol.wait;" ::: "memory");

@@ -69,8 +69,8 @@ struct AttnArgs {
   float* lse;             // optional [n_query, H]
   int qk_waits_pv;        // tcgen05 kernel: Q K^T of tile i+1 waits for the completion barrier of P V of tile i-1
   int gather4;            // tcgen05 kernel: scattered rows by TMA gather (cp.async.bulk.tensor tile::gather4) where the cache allows
-  int rows_stable;        // tcgen05 kernel, row lists: `rows` / `n_rows` were complete before the previous kernel of the
-                          // stream started, so they may be read ahead of the programmatic dependency wait
+  int rows_stable;        // tcgen05 kernel, row lists: `rows` / `n_rows` and the cache were complete before the previous kernel of
+                          // the stream started, so they may be read ahead of the programmatic dependency wait
   int sm_count;           // tcgen05 kernel: blocks that run at the same time
   int n_split;            // >1: partial results in part_out / part_lse, merged afterwards
   int v_shift;            // tcgen05 kernel, 16 splits only: the value dims in 2^v_shift parts (0, 1 or 2)

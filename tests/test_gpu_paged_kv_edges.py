@@ -71,3 +71,38 @@ def test_append_without_a_workspace_is_refused(cuda_device):
     finally:
         ctx.h = with_workspace
         binding.lib().lsa_destroy(bare)
+
+
+def test_sparse_attention_right_after_an_append_of_another_context(cuda_device):
+    """The row lists stay, the rows do not: each step's append writes every sequence's last row, and the attention launched right behind
+    it, on the lists of the attention before, reads the new one."""
+    from paper_2608_01662_b200.configs import CONFIGS
+    from paper_2608_01662_b200.workload import DecodeWorkload
+    cfg = CONFIGS["cfg4"].replace(batch=64, ctx_lo=300, ctx_hi=3000, M=64, Ksp=1024, R=1)
+    wl = DecodeWorkload(cfg, cuda_device)
+    wl.prepare()
+    wl.step()
+    rows = torch.empty((cfg.batch, cfg.S + cfg.Ksp + cfg.W), dtype=torch.int32, device=cuda_device)
+    n_rows = torch.empty((cfg.batch,), dtype=torch.int32, device=cuda_device)
+    wl.ctx.convert(wl.sparse_idx, wl.n_sparse, 0, cfg.batch, rows, n_rows, None, wl.page_table, wl.ctx_len)
+    kv = binding.Context(None, 0, 0, device=cuda_device, kv=binding.make_kv_params(64, 1, 576, 512, cfg.kv_page, latent=True))
+    steps, before = 24, wl.ctx_len - 1
+    gen = torch.Generator(cuda_device).manual_seed(38)
+    new = torch.randn(steps, cfg.batch, 576, generator=gen, device=cuda_device).mul(3).to(torch.bfloat16)
+    pool = wl.k[0].view(-1, wl.k[0].shape[-1])
+
+    def step(s, out):
+        kv.kv_append(new[s].view(cfg.batch, 1, 576), None, pool, None, wl.page_table, before)
+        wl.ctx.sparse_attn(wl.q[0], wl.k[0], wl.v[0], wl.sparse_idx, wl.n_sparse, 0, cfg.batch, 0, out, None, rows, n_rows, wl.ctx_len, cfg.batch)
+    outs = torch.empty(2, steps, *wl.out[0].shape, dtype=torch.bfloat16, device=cuda_device)
+    torch.cuda.synchronize()
+    for s in range(steps):
+        step(s, outs[0, s])
+    assert wl.ctx.status() == 0 and kv.status() == 0
+    for s in range(steps):
+        kv.kv_append(new[s].view(cfg.batch, 1, 576), None, pool, None, wl.page_table, before)
+        torch.cuda.synchronize()
+        step(s, outs[1, s])
+        torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1])
+    assert not torch.equal(outs[0, 0], outs[0, 1])
