@@ -201,24 +201,26 @@ _contexts: dict = {}
 
 def _context(s):
     """The library's handle, which a program keeps per stream for the shapes that it serves (its calls go to the stream it was made for)."""
+    device = s["q"].get_device()
+    stream = torch._C._cuda_getCurrentRawStream(device)   # (a number: torch.cuda.current_stream makes an object, 2 us a call)
+    ctx = _contexts.get((s.get("kv_bytes"), device, stream))
+    return ctx if ctx is not None else _new_context(s, device, stream)
+
+
+def _new_context(s, device, stream):
     from paper_2608_01662_b200 import binding
 
-    kv = s.get("kv")
-    if kv is None:
-        c = s["case"]
-        kv = s["kv"] = binding.make_kv_params(n_heads=c["heads"], n_kv_heads=c["kv_heads"], d_qk=c["d_qk"], d_v=_d_v(c), latent=c["latent"],
-                                              dtype=c["dtype"], e4m3=c["e4m3"], kv_page=c["page"], d_rope=c.get("d_rope", 0),
-                                              rope_at=c["d_qk"] - 64 if c["latent"] and c["op"] == "append" else 0,
-                                              rope_interleaved=c.get("interleaved", False), sink=c.get("sink", 0), window=c.get("window", 0),
-                                              sm_scale=c["d_qk"] ** -0.5)
-        s["kv_bytes"] = bytes(kv)
-    device = s["q"].device
-    stream = torch.cuda.current_stream(device)
-    key = (s["kv_bytes"], device, stream.cuda_stream)
-    ctx = _contexts.get(key)
-    if ctx is None:
-        ctx = _contexts[key] = binding.Context(None, 0, 0, device=device, stream=stream, kv=kv)
-    return ctx
+    c = s["case"]
+    kv = binding.make_kv_params(n_heads=c["heads"], n_kv_heads=c["kv_heads"], d_qk=c["d_qk"], d_v=_d_v(c), latent=c["latent"], dtype=c["dtype"],
+                                e4m3=c["e4m3"], kv_page=c["page"], d_rope=c.get("d_rope", 0),
+                                rope_at=c["d_qk"] - 64 if c["latent"] and c["op"] == "append" else 0,
+                                rope_interleaved=c.get("interleaved", False), sink=c.get("sink", 0), window=c.get("window", 0),
+                                sm_scale=c["d_qk"] ** -0.5)
+    s["kv_bytes"] = bytes(kv)
+    key = (s["kv_bytes"], device, stream)
+    if key not in _contexts:
+        _contexts[key] = binding.Context(None, 0, 0, device=s["q"].device, kv=kv)   # (on the current stream)
+    return _contexts[key]
 
 
 def run(state):
