@@ -165,7 +165,8 @@ LSA_API int lsa_tune(lsa_ctx* ctx, int knob, int value);
  * launches go unrecorded).  lsa_profile_read waits for the stream and writes, per class, the summed
  * device time in ms and the number of recorded launches (host arrays of LSA_K_COUNT entries), then
  * starts over.  The first enable creates the events (host resources only). */
-/* lsa_append is timed as LSA_K_MEANS */
+/* lsa_append and lsa_kv_append are timed as LSA_K_MEANS, lsa_paged_attn (both of its launches together) as LSA_K_ATTN: a context that
+ * serves the sparse path too has both in these sums */
 enum { LSA_K_MEANS = 0, LSA_K_COARSE, LSA_K_FINE_SELECT, LSA_K_SELECT, LSA_K_CONVERT, LSA_K_ATTN, LSA_K_MERGE, LSA_K_COUNT };   /* lsa_merge is timed as LSA_K_MERGE */
 LSA_API int lsa_profile_enable(lsa_ctx* ctx, int on);
 LSA_API int lsa_profile_read(lsa_ctx* ctx, double* total_ms, int64_t* launches);

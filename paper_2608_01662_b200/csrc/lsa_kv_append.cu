@@ -6,8 +6,11 @@
 // row's threads are consecutive lanes, so the largest element of an e4m3 row is a few shuffles.
 //
 // Bound: HBM for prompts (read and write once: 17 thousand tokens, 32 query and 8 KV heads of 128, 70 us, 0.94 of a copy's rate; 9871
-// tokens, 64 query heads, e4m3 caches 68 us, 0.87), a launch and the chain length -> page -> row for decode steps (3 to 5 us).  Rows are
+// tokens, 64 query heads, e4m3 caches 67 us, 0.88), a launch and the chain length -> page -> row for decode steps (3 to 5 us).  Rows are
 // on their way before the token's place is known, and no load stands behind a branch (with branches around the loads: 90 us, not 69).
+// Between the two, and for narrow tokens, it is the chain of a block, which lives for one token: 5000 tokens of latent rows 133 us with 64
+// heads (0.86 of a copy's rate), 51 with 16 (0.60); 400 tokens 15.3 (0.60) and 4.9 (0.50); 5000 of 32 over 8 heads 24.5 (0.78), into
+// codes 27.9 (0.63).
 #include <algorithm>
 
 #include "lsa_paged.cuh"
@@ -86,8 +89,10 @@ constexpr int kFewTokens = D == 576 ? 576 : 512;
 template <int D>
 constexpr int kManyTokens = D == 576 ? 288 : 64;
 // Query rows that a thread has on their way at a time: four, or two where the block's threads then have all of them, and more blocks
-// fit an SM (5000 tokens of latent rows: 16 heads 65 us by four, 51 by two; 64 heads 134, 139).  A block of 288 threads is nine warps, so
-// that of two one SM partition has five: they fit with 96 registers each, which is what a bound of two blocks of ten warps gives.
+// fit an SM (latent rows of 16 heads: 5000 tokens 65 us by four, 51 by two, 250 tokens 4.2, 4.7; 64 heads, 5000 tokens: 134, 139).  A
+// block of 288 threads is nine warps, so that of two one SM partition has five: they fit with 96 registers each, which is what a bound of
+// two blocks of ten warps gives.  Three blocks with two rows a thread have 64 registers: 32 to 52 bytes a thread go to memory and back,
+// once a token; 16 bytes in the block of 576 threads (96 registers).
 template <int kThreads>
 constexpr int kBound = kThreads == 288 ? 320 : kThreads;
 template <int kThreads, int kQAtOnce>

@@ -1,7 +1,7 @@
 // lsa_paged_attn for caches with separate keys and values: one query per sequence, up to 16 query heads per KV head.
 //
-// A query head's 64 or 128 dims meet each cached key and value once: at most 16 flop per byte read, so the kernel has to keep
-// HBM busy and everything else has to stay out of its way.  Both products are m16n8k16 MMAs with the cache as the A operand and the
+// A query head's 64 or 128 dims meet each cached key and value once: at most 16 flop per byte read (32 where it is a code), so the
+// kernel has to keep HBM busy and everything else has to stay out of its way.  Both products are m16n8k16 MMAs with the cache as the A operand and the
 // heads as the eight columns: S^T = K Q^T (16 tokens x 8 heads) and O^T = V^T P^T (16 dims x 8 heads).  The other way round the
 // heads are 16 rows, of which groups of 4 or 8 heads leave most empty: twice the MMAs and twice the registers of O.
 //
@@ -22,6 +22,11 @@
 // the largest product still has all its bits.  (With weights times scales in bf16 and codes turned into bf16 139 to 146 us instead
 // of 137, and a third more error.)  The conversions of codes keep these caches at 0.86 of a copy's rate (32 sequences of up to 32
 // thousand tokens, 64 query and 8 KV heads, 774 MB in 137 us).
+//
+// 9 to 16 query heads per KV head are two groups of columns, the products and the softmax of each strip twice; that shows most where a
+// strip is few bytes: 99 thousand tokens of 128 over 8 heads 83 us in bf16 (0.75 of a copy's rate), 70 as codes (0.45); 688 thousand of
+// 16 over 1 head 42 us with 64 dims in bf16 (0.64), 68 with 128 dims as codes (0.41; there 60 to 92 bytes a thread do not fit the 168
+// registers).
 #include "lsa_paged.cuh"
 #include "lsa_tc.cuh"
 
